@@ -89,7 +89,8 @@ typedef enum FA_ENUM_BASE {
     FA_ERR_WORKSPACE = 10,   /* workspace allocation failed or not allowed (stream capture), or a caller-owned one is too small */
     FA_ERR_HIP = 11,         /* a HIP runtime call or kernel launch failed */
     FA_ERR_SPLITS = 12,      /* num_splits outside [0, FA_MAX_SPLITS] */
-    FA_ERR_PACKING = 13      /* slots or heads per workgroup not allowed (see fa_fwd_slots) */
+    FA_ERR_PACKING = 13,     /* slots or heads per workgroup not allowed (see fa_fwd_slots) */
+    FA_ERR_ROTARY = 14       /* rotary description not allowed (see fa_rotary_t) */
 } fa_status_t;
 
 #define FA_MAX_SPLITS 256
@@ -362,6 +363,78 @@ size_t fa_unfused_workspace_bytes(int B, int Hq, int Nq, int Nk);
  * or x, FA_ERR_HIP when the launch fails. */
 fa_status_t fa_q8_0_gemv(const void *w, const void *x, void *y, int M, int K, fa_dtype_t x_dtype,
                          fa_dtype_t y_dtype, void *stream);
+
+/* Rotation of queries and keys by their positions, as fa_kvcache_append
+ * applies it.  Of a head's D columns the first rot_dim rotate, in pairs: the
+ * pair j at position p turns by t = p * inv_freq[j] radians,
+ *   (a, b) -> (a cos t - b sin t, a sin t + b cos t).
+ * t is formed in 64 bits; the rotation is computed in fp32 and rounded once.
+ *   inv_freq   device, rot_dim / 2 floats: radians per position of each pair
+ *   positions  device int32 [axes][B][Nq]: the tokens' positions on each axis
+ *              (time, height and width of a picture's patches, say; any int32),
+ *              or NULL: the tokens' rows in the cache (one axis)
+ *   rot_dim    even, 2 .. D
+ *   interleaved  0: pair j is columns j and j + rot_dim / 2; else 2 j and 2 j + 1
+ *   axes       1 .. FA_MAX_AXES; more than 1 needs positions
+ *   pair_axis  axis whose position turns pair j (host array, read with the
+ *              call; ignored with one axis) */
+#define FA_MAX_AXES 4
+#define FA_MAX_ROTARY_PAIRS 128
+typedef struct {
+    const float *inv_freq;
+    const int *positions;
+    int rot_dim;
+    int interleaved;
+    int axes;
+    unsigned char pair_axis[FA_MAX_ROTARY_PAIRS];
+} fa_rotary_t;
+
+/* New keys and values into the caches that fa_fwd_kvcache reads, and the new
+ * queries made ready for it, in one kernel.  The Nq new tokens of batch element
+ * b are the last of its seqlens_k[b] keys (the lengths fa_fwd_kvcache is given
+ * next): token i goes to cache row seqlens_k[b] - Nq + i.  Rows below 0 (a
+ * sequence with fewer new tokens: its first ones are padding) and from Nk on
+ * are not written; no other row is touched.
+ *   k, v    [B][Nq][Hkv][D] new keys and values; k_stride, v_stride elements
+ *           lie between consecutive tokens (0: Hkv * D), so that they may be
+ *           parts of one projection's result; heads and columns are dense
+ *   k_cache, v_cache  [B][Nk][Hkv][D] dense; k rotated, v as it is
+ *   q       [B][Nq][Hq][D] new queries, q_stride elements between tokens
+ *           (0: Hq * D), or NULL (q_out too; Hq is then ignored)
+ *   q_out   [B][Nq][Hq][D] dense: q rotated, padding tokens' included; q
+ *           itself where q is dense
+ *   rotary  host, read with the call; NULL: nothing rotates
+ * dtype is that of all of them (fp16, bf16 or fp32).  Allocates nothing.
+ * Errors (before any HIP call): FA_ERR_NULL for a NULL k, v, cache, length
+ * array or inv_freq, or one of q and q_out alone; FA_ERR_DIM for a size < 1,
+ * a stride below the row or sizes too large ((Hq + 2 Hkv) * D above 2^28, B *
+ * Nq above 2^31 - 1); FA_ERR_DTYPE; FA_ERR_GQA_RATIO (with q); FA_ERR_HEAD_DIM
+ * for D not a multiple of 8 or above 256; FA_ERR_ROTARY for a rot_dim, axes or
+ * pair_axis out of range or several axes without positions; FA_ERR_ALIGN for a
+ * tensor pointer or token stride not a multiple of 16 bytes, an int32 or float
+ * array not of 4; FA_ERR_ALIAS when an output (q_out, k_cache, v_cache) overlaps
+ * an input or another output (but q_out being q). */
+fa_status_t fa_kvcache_append(const void *k, const void *v, void *k_cache, void *v_cache,
+                              const void *q, void *q_out, const int *seqlens_k, int B, int Hq,
+                              int Hkv, int Nq, int Nk, int D, long long q_stride,
+                              long long k_stride, long long v_stride, const fa_rotary_t *rotary,
+                              void *stream, fa_dtype_t dtype);
+
+/* fa_kvcache_append into the paged cache of fa_fwd_kvcache_paged: row j of
+ * batch element b is row j % page_size of page block_table[b][j / page_size].
+ * A token whose table entry lies outside [0, num_pages) is not written, nor is
+ * one past page_size * max_pages rows; the pages that a call writes to must be
+ * the tokens' own (two tokens that name one row leave either's values there).
+ * fp16, bf16 and fp32, any D that fa_kvcache_append takes.  Errors: those of
+ * fa_kvcache_append, FA_ERR_NULL for a NULL table, FA_ERR_DIM for page_size not a
+ * positive multiple of 64, max_pages or num_pages < 1 or page_size * max_pages
+ * or B * max_pages above 2^31 - 1. */
+fa_status_t fa_kvcache_append_paged(const void *k, const void *v, void *k_pages, void *v_pages,
+                                    const void *q, void *q_out, const int *seqlens_k,
+                                    const int *block_table, int B, int Hq, int Hkv, int Nq, int D,
+                                    int page_size, int max_pages, int num_pages,
+                                    long long q_stride, long long k_stride, long long v_stride,
+                                    const fa_rotary_t *rotary, void *stream, fa_dtype_t dtype);
 
 #ifdef __cplusplus
 }

@@ -6,13 +6,14 @@ HIP library is loaded on first use and its absence raises (no CPU fallback).
 """
 from __future__ import annotations
 
+import ctypes
 import math
 
 from . import _lib
 
 __all__ = ["fwd", "fwd_splitkv", "fwd_splitkv_noalloc", "fwd_kvcache", "fwd_kvcache_paged", "fwd_unfused",
            "unfused_workspace_bytes", "q8_0_gemv", "FaError", "validate", "workspace_bytes", "release_workspace",
-           "set_workspace", "version", "DTYPE_CODES"]
+           "set_workspace", "version", "DTYPE_CODES", "kvcache_append", "kvcache_append_paged"]
 
 
 class FaError(RuntimeError):
@@ -287,6 +288,121 @@ def fwd_kvcache_paged(q, k_pages, v_pages, block_table, seqlens_k, causal: bool 
     else:
         _call(rt, lib, index, lib.fa_fwd_kvcache_paged, args)
     return out, lse
+
+
+def _token_stride(t, name):
+    """Elements between the consecutive tokens of t [B, N, H, D], whose heads and
+    columns are dense and whose sequences follow each other."""
+    B, N, H, D = t.shape
+    sb, sn, sh, sd = t.stride()
+    step = sn if N > 1 else sb if B > 1 else H * D
+    if ((sd != 1 and D > 1) or (sh != D and H > 1) or (N > 1 and B > 1 and sb != N * sn) or step < H * D):
+        raise ValueError(f"{name} must be [B, N, H, D] with dense heads and one stride between its tokens")
+    return step
+
+
+def _rotary(rt, inv_freq, positions, pair_axes, interleaved, B, N, device):
+    """The fa_rotary_t of a call (None: no rotation)."""
+    if inv_freq is None:
+        if positions is not None or pair_axes is not None:
+            raise ValueError("positions and pair_axes need inv_freq")
+        return None
+    if (inv_freq.dtype != rt.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous()
+            or inv_freq.device != device):
+        raise ValueError("inv_freq must be a contiguous float32 [rot_dim / 2] tensor on k's device")
+    pairs, axes = inv_freq.shape[0], 1
+    r = _lib.Rotary(inv_freq.data_ptr(), None, 2 * pairs, 1 if interleaved else 0, 1)
+    if positions is not None:
+        shape = tuple(positions.shape)
+        if (positions.dtype != rt.int32 or not positions.is_contiguous() or positions.device != device
+                or shape[-2:] != (B, N) or len(shape) > 3):
+            raise ValueError("positions must be a contiguous int32 [B, N] or [axes, B, N] tensor on k's device")
+        axes = shape[0] if len(shape) == 3 else 1
+        r.positions, r.axes = positions.data_ptr(), axes
+    if axes > 1:
+        if pair_axes is None or len(pair_axes) != pairs:
+            raise ValueError("several axes need pair_axes, the axis of each of the rot_dim / 2 pairs")
+        if pairs <= _lib.FA_MAX_ROTARY_PAIRS:   # (more are refused by the call)
+            ctypes.memmove(r.pair_axis, bytes(pair_axes), pairs)
+    return r
+
+
+def _append(k, v, k_cache, v_cache, block_table, seqlens_k, q, q_out, rotary):
+    lib = _lib.load()
+    rt = _runtime()
+    dt, dev = k.dtype, k.device
+    if not k.is_cuda or k.dim() != 4 or dt not in rt.codes:
+        raise ValueError("k must be a 4-D [B, N, Hkv, D] GPU tensor of float16, bfloat16 or float32")
+    if v.shape != k.shape or v.dtype != dt or v.device != dev:
+        raise ValueError("v must have k's shape, dtype and device")
+    B, N, Hkv, D = k.shape
+    for name, t in (("k", k_cache), ("v", v_cache)):
+        if t.dim() != 4 or not t.is_contiguous() or t.dtype != dt or t.device != dev:
+            raise ValueError(f"the {name} cache must be contiguous and 4-D, of k's dtype and device")
+    first, rows, ch, cd = k_cache.shape
+    if v_cache.shape != k_cache.shape or ch != Hkv or cd != D or (block_table is None and first != B):
+        raise ValueError("the caches must have one shape, with k's heads and head size")
+    if (seqlens_k.dtype != rt.int32 or tuple(seqlens_k.shape) != (B,) or not seqlens_k.is_contiguous()
+            or seqlens_k.device != dev):
+        raise ValueError("seqlens_k must be a contiguous int32 [B] tensor on k's device")
+    Hq, qs = 0, 0
+    if q is not None:
+        if q.dim() != 4 or q.dtype != dt or q.device != dev or q.shape[:2] != k.shape[:2] or q.shape[3] != D:
+            raise ValueError("q must be [B, N, Hq, D] with k's B, N, D, dtype and device")
+        Hq, qs = q.shape[2], _token_stride(q, "q")
+        if q_out is None:
+            q_out = rt.torch.empty(q.shape, dtype=dt, device=dev)
+        elif q_out.shape != q.shape or q_out.dtype != dt or not q_out.is_contiguous() or q_out.device != dev:
+            raise ValueError("q_out must be a contiguous tensor of q's shape, dtype and device")
+    elif q_out is not None:
+        raise ValueError("q_out needs q")
+    index = dev.index
+    ptrs = (k.data_ptr(), v.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+            q.data_ptr() if q is not None else None, q_out.data_ptr() if q is not None else None, seqlens_k.data_ptr())
+    r = _rotary(rt, *rotary, B, N, dev)
+    tail = (qs, _token_stride(k, "k"), _token_stride(v, "v"), ctypes.addressof(r) if r is not None else None,
+            rt.stream(index), rt.codes[dt])
+    if block_table is None:
+        _call(rt, lib, index, lib.fa_kvcache_append, (*ptrs, B, Hq, Hkv, N, rows, D, *tail))
+    else:
+        if (block_table.dtype != rt.int32 or block_table.dim() != 2 or block_table.shape[0] != B
+                or not block_table.is_contiguous() or block_table.device != dev):
+            raise ValueError("block_table must be a contiguous int32 [B, max_pages] tensor on k's device")
+        _call(rt, lib, index, lib.fa_kvcache_append_paged,
+              (*ptrs, block_table.data_ptr(), B, Hq, Hkv, N, D, rows, block_table.shape[1], first, *tail))
+    return q_out
+
+
+def kvcache_append(k, v, k_cache, v_cache, seqlens_k, q=None, q_out=None, inv_freq=None, positions=None,
+                   pair_axes=None, interleaved: bool = False):
+    """Write new keys and values into the caches that ``fwd_kvcache`` reads and
+    rotate them, and the new queries, by their positions (fa_kvcache_append).
+
+    ``k``, ``v`` [B, N, Hkv, D] are the last N of each sequence's ``seqlens_k``
+    (int32 [B], the new tokens included) keys: token i goes to row seqlens_k[b] -
+    N + i of the contiguous ``k_cache``, ``v_cache`` [B, Nk, Hkv, D]; rows below
+    0 (padding) and past the cache are not written.  ``k``, ``v`` and ``q``
+    [B, N, Hq, D] may be parts of one projection's result (dense heads, one
+    stride between tokens).  ``inv_freq`` (float32 [rot_dim / 2], None: no
+    rotation): radians per position of each pair of columns, j and j + rot_dim /
+    2, or 2 j and 2 j + 1 if ``interleaved``.  ``positions``: int32 [B, N], or
+    [axes, B, N] with ``pair_axes``, the axis that turns each pair (bytes or a
+    sequence of ints); None: the cache rows.  Returns the rotated queries
+    (``q_out`` if given, which may be ``q`` if that is contiguous; None without
+    ``q``)."""
+    return _append(k, v, k_cache, v_cache, None, seqlens_k, q, q_out, (inv_freq, positions, pair_axes, interleaved))
+
+
+def kvcache_append_paged(k, v, k_pages, v_pages, block_table, seqlens_k, q=None, q_out=None, inv_freq=None,
+                         positions=None, pair_axes=None, interleaved: bool = False):
+    """``kvcache_append`` into the paged cache of ``fwd_kvcache_paged``: ``k_pages``,
+    ``v_pages`` [num_pages, page_size, Hkv, D], ``block_table`` int32 [B,
+    max_pages].  Tokens whose table entry is outside the pool are not written
+    (fa_kvcache_append_paged)."""
+    if block_table is None:
+        raise ValueError("block_table must be a contiguous int32 [B, max_pages] tensor on k's device")
+    return _append(k, v, k_pages, v_pages, block_table, seqlens_k, q, q_out,
+                   (inv_freq, positions, pair_axes, interleaved))
 
 
 def q8_0_gemv(w, x, out=None, out_dtype=None):

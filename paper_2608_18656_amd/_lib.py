@@ -19,7 +19,7 @@ STATUS_NAMES = {
     0: "FA_OK", 1: "FA_ERR_NULL", 2: "FA_ERR_DIM", 3: "FA_ERR_GQA_RATIO", 4: "FA_ERR_HEAD_DIM",
     5: "FA_ERR_CAUSAL_SHAPE", 6: "FA_ERR_SCALE", 7: "FA_ERR_ALIGN", 8: "FA_ERR_ALIAS",
     9: "FA_ERR_DTYPE", 10: "FA_ERR_WORKSPACE", 11: "FA_ERR_HIP", 12: "FA_ERR_SPLITS",
-    13: "FA_ERR_PACKING",
+    13: "FA_ERR_PACKING", 14: "FA_ERR_ROTARY",
 }
 
 # Every symbol include/fa.h declares.
@@ -27,7 +27,8 @@ EXPORTS = ("fa_status_string", "fa_version", "fa_validate", "fa_fwd_f16", "fa_fw
            "fa_fwd_f32", "fa_fwd", "fa_fwd_splitkv", "fa_workspace_bytes",
            "fa_release_workspace", "fa_set_workspace", "fa_fwd_packed", "fa_fwd_kvcache",
            "fa_q8_0_gemv", "fa_fwd_kvcache_paged", "fa_fwd_unfused", "fa_unfused_workspace_bytes",
-           "fa_fwd_ws", "fa_fwd_kvcache_ws", "fa_fwd_kvcache_paged_ws", "fa_fwd_splitkv_noalloc", "fa_fwd_slots")
+           "fa_fwd_ws", "fa_fwd_kvcache_ws", "fa_fwd_kvcache_paged_ws", "fa_fwd_splitkv_noalloc", "fa_fwd_slots",
+           "fa_kvcache_append", "fa_kvcache_append_paged")
 
 _lib = None
 
@@ -35,6 +36,16 @@ _P = ctypes.c_void_p
 _I = ctypes.c_int
 _F = ctypes.c_float
 _DIMS = [_I] * 7 + [_F]
+
+
+FA_MAX_AXES, FA_MAX_ROTARY_PAIRS = 4, 128
+_L = ctypes.c_longlong
+
+
+class Rotary(ctypes.Structure):
+    """fa_rotary_t."""
+    _fields_ = [("inv_freq", _P), ("positions", _P), ("rot_dim", _I), ("interleaved", _I), ("axes", _I),
+                ("pair_axis", ctypes.c_ubyte * FA_MAX_ROTARY_PAIRS)]
 
 
 def load():
@@ -90,5 +101,9 @@ def load():
     lib.fa_fwd_kvcache_paged_ws.argtypes = ([_P] * 7 + [_I] * 9 + [ctypes.c_float, _P, _I, _I, _P,
                                                                    ctypes.c_size_t])
     lib.fa_fwd_kvcache_paged_ws.restype = _I
+    lib.fa_kvcache_append.argtypes = [_P] * 7 + [_I] * 6 + [_L] * 3 + [_P, _P, _I]
+    lib.fa_kvcache_append.restype = _I
+    lib.fa_kvcache_append_paged.argtypes = [_P] * 8 + [_I] * 8 + [_L] * 3 + [_P, _P, _I]
+    lib.fa_kvcache_append_paged.restype = _I
     _lib = lib
     return lib

@@ -199,6 +199,9 @@ const char *fa_status_string(fa_status_t s) {
     case FA_ERR_PACKING:
         return "FA_ERR_PACKING: slots_per_workgroup must be 0, 1, 2, 4 or 8; heads_per_workgroup 0, 1, 2, 4 or "
                "8, dividing Hq / Hkv and the slots";
+    case FA_ERR_ROTARY:
+        return "FA_ERR_ROTARY: rot_dim must be even, 2 to D; axes 1 to 4, with positions if several, and pair_axis "
+               "below axes";
     }
     return "unknown fa_status_t";
 }
@@ -273,15 +276,33 @@ fa_status_t kvcache(const void *q, const void *k, const void *v, void *o, float 
                0, seqlens_k, Paging(), cws);
 }
 
+bool pages_ok(int B, int page_size, int max_pages, int num_pages) {
+    return page_size >= 64 && page_size % 64 == 0 && max_pages >= 1 && num_pages >= 1 &&
+           (long long)page_size * max_pages <= 0x7fffffffLL && (long long)B * max_pages <= 0x7fffffffLL;
+}
+
+fa_status_t append(const void *k, const void *v, void *k_cache, void *v_cache, const void *q, void *q_out,
+                   const int *seqlens, int B, int Hq, int Hkv, int N, int Nk, int D, long long qs, long long ks,
+                   long long vs, const fa_rotary_t *rotary, void *stream, fa_dtype_t dtype, const Paging &pg) {
+    if (qs == 0) qs = (long long)Hq * D;
+    if (ks == 0) ks = (long long)Hkv * D;
+    if (vs == 0) vs = (long long)Hkv * D;
+    const long long rows = pg.block_table ? (long long)pg.num_pages * pg.page_size : (long long)B * Nk;
+    const fa_status_t st = fa::validate_append(k, v, k_cache, v_cache, q, q_out, seqlens, B, Hq, Hkv, N, D, qs, ks, vs,
+                                               rotary, dtype, rows, pg.block_table, pg.max_pages);
+    if (st != FA_OK) return st;
+    const fa::AppendProblem p{k, v, k_cache, v_cache, q, q_out, seqlens, B, Hq, Hkv, N, Nk, D, qs, ks, vs, rotary,
+                              dtype, pg.block_table, pg.page_size, pg.max_pages, pg.num_pages};
+    return fa::launch_append(p, reinterpret_cast<hipStream_t>(stream)) == hipSuccess ? FA_OK : FA_ERR_HIP;
+}
+
 fa_status_t kvcache_paged(const void *q, const void *k_pages, const void *v_pages, void *o,
                           float *lse, const int *seqlens_k, const int *block_table, int B, int Hq,
                           int Hkv, int Nq, int D, int page_size, int max_pages, int num_pages,
                           int causal, float scale, void *stream, fa_dtype_t in_dtype,
                           fa_dtype_t out_dtype, const CallWs *cws) {
     if (!seqlens_k || !block_table) return FA_ERR_NULL;
-    if (page_size < 64 || page_size % 64 != 0 || max_pages < 1 || num_pages < 1 ||
-        (long long)page_size * max_pages > 0x7fffffffLL || (long long)B * max_pages > 0x7fffffffLL)
-        return FA_ERR_DIM;
+    if (!pages_ok(B, page_size, max_pages, num_pages)) return FA_ERR_DIM;
     if ((reinterpret_cast<uintptr_t>(seqlens_k) & 3) || (reinterpret_cast<uintptr_t>(block_table) & 3))
         return FA_ERR_ALIGN;
     const int Nk = page_size * max_pages;
@@ -432,6 +453,30 @@ fa_status_t fa_q8_0_gemv(const void *w, const void *x, void *y, int M, int K, fa
     const hipError_t e =
         fa::launch_q8_gemv(w, x, y, M, K, x_dtype, y_dtype, reinterpret_cast<hipStream_t>(stream));
     return e == hipSuccess ? FA_OK : FA_ERR_HIP;
+}
+
+fa_status_t fa_kvcache_append(const void *k, const void *v, void *k_cache, void *v_cache, const void *q,
+                              void *q_out, const int *seqlens_k, int B, int Hq, int Hkv, int Nq, int Nk, int D,
+                              long long q_stride, long long k_stride, long long v_stride,
+                              const fa_rotary_t *rotary, void *stream, fa_dtype_t dtype) {
+    return append(k, v, k_cache, v_cache, q, q_out, seqlens_k, B, Hq, Hkv, Nq, Nk, D, q_stride, k_stride, v_stride,
+                  rotary, stream, dtype, Paging());
+}
+
+fa_status_t fa_kvcache_append_paged(const void *k, const void *v, void *k_pages, void *v_pages, const void *q,
+                                    void *q_out, const int *seqlens_k, const int *block_table, int B, int Hq,
+                                    int Hkv, int Nq, int D, int page_size, int max_pages, int num_pages,
+                                    long long q_stride, long long k_stride, long long v_stride,
+                                    const fa_rotary_t *rotary, void *stream, fa_dtype_t dtype) {
+    if (!block_table) return FA_ERR_NULL;
+    if (!pages_ok(B, page_size, max_pages, num_pages)) return FA_ERR_DIM;
+    Paging pg;
+    pg.block_table = block_table;
+    pg.page_size = page_size;
+    pg.max_pages = max_pages;
+    pg.num_pages = num_pages;
+    return append(k, v, k_pages, v_pages, q, q_out, seqlens_k, B, Hq, Hkv, Nq, page_size * max_pages, D, q_stride,
+                  k_stride, v_stride, rotary, stream, dtype, pg);
 }
 
 size_t fa_unfused_workspace_bytes(int B, int Hq, int Nq, int Nk) {

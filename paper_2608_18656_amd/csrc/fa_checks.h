@@ -69,4 +69,69 @@ inline fa_status_t validate_core(const void *q, const void *k, const void *v, co
     return FA_OK;
 }
 
+inline bool misaligned(const void *p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) != 0; }
+
+// A range of memory that a call reads or writes.
+struct Range {
+    const void *p;
+    size_t bytes;
+};
+
+// The argument checks of fa_kvcache_append (table NULL) and its paged form.
+// cache_rows: rows of Hkv * D elements that each cache holds.  Strides are
+// those in use (0 already replaced).
+inline fa_status_t validate_append(const void *k, const void *v, const void *k_cache, const void *v_cache,
+                                   const void *q, const void *q_out, const int *seqlens, int B, int Hq, int Hkv,
+                                   int N, int D, long long qs, long long ks, long long vs, const fa_rotary_t *rotary,
+                                   fa_dtype_t dtype, long long cache_rows, const int *table, int max_pages) {
+    if (!k || !v || !k_cache || !v_cache || !seqlens || (q == nullptr) != (q_out == nullptr) ||
+        (rotary && !rotary->inv_freq))
+        return FA_ERR_NULL;
+    if (B < 1 || Hkv < 1 || (q && Hq < 1) || N < 1 || cache_rows < 1 || D < 1) return FA_ERR_DIM;
+    if (dtype != FA_F16 && dtype != FA_BF16 && dtype != FA_F32) return FA_ERR_DTYPE;
+    if (q && Hq % Hkv != 0) return FA_ERR_GQA_RATIO;
+    if (D % 8 != 0 || D > 256) return FA_ERR_HEAD_DIM;
+    const long long heads = (q ? Hq : 0) + 2LL * Hkv, tokens = (long long)B * N;
+    if (heads * D > (1LL << 28) || tokens > 0x7fffffffLL) return FA_ERR_DIM;
+    if ((q && qs < (long long)Hq * D) || ks < (long long)Hkv * D || vs < (long long)Hkv * D) return FA_ERR_DIM;
+    long long nq = 0, nk, nv, nc;
+    if ((q && !mul_ok(tokens, qs, &nq)) || !mul_ok(tokens, ks, &nk) || !mul_ok(tokens, vs, &nv) ||
+        !mul_ok(cache_rows, (long long)Hkv * D, &nc))
+        return FA_ERR_DIM;
+    if (rotary) {
+        if (rotary->rot_dim < 2 || rotary->rot_dim % 2 != 0 || rotary->rot_dim > D || rotary->axes < 1 ||
+            rotary->axes > FA_MAX_AXES || (rotary->axes > 1 && !rotary->positions))
+            return FA_ERR_ROTARY;
+        if (rotary->axes > 1)
+            for (int j = 0; j < rotary->rot_dim / 2; ++j)
+                if (rotary->pair_axis[j] >= rotary->axes) return FA_ERR_ROTARY;
+    }
+    const long long e = (long long)esize(dtype);
+    if (misaligned(k, 16) || misaligned(v, 16) || misaligned(k_cache, 16) || misaligned(v_cache, 16) ||
+        misaligned(q, 16) || misaligned(q_out, 16) || misaligned(seqlens, 4) || misaligned(table, 4) ||
+        (rotary && (misaligned(rotary->inv_freq, 4) || misaligned(rotary->positions, 4))) || (q && qs * e % 16 != 0) ||
+        ks * e % 16 != 0 || vs * e % 16 != 0)
+        return FA_ERR_ALIGN;
+    const size_t dense = (size_t)tokens * Hq * D * e, cb = (size_t)(nc * e);
+    const Range in[] = {{k, (size_t)((nk - ks + (long long)Hkv * D) * e)},
+                        {v, (size_t)((nv - vs + (long long)Hkv * D) * e)},
+                        {q, q ? (size_t)((nq - qs + (long long)Hq * D) * e) : 0},
+                        {seqlens, (size_t)B * sizeof(int)},
+                        {table, table ? (size_t)B * max_pages * sizeof(int) : 0},
+                        {rotary ? rotary->inv_freq : nullptr, rotary ? (size_t)rotary->rot_dim / 2 * sizeof(float) : 0},
+                        {rotary ? rotary->positions : nullptr,
+                         rotary && rotary->positions ? (size_t)rotary->axes * tokens * sizeof(int) : 0}};
+    const Range out[] = {{k_cache, cb}, {v_cache, cb}, {q_out, q ? dense : 0}};
+    for (int i = 0; i < 3; ++i) {
+        if (!out[i].bytes) continue;
+        for (const Range &r : in) {
+            if (!r.bytes || (i == 2 && r.p == q && q == q_out && qs == (long long)Hq * D)) continue;
+            if (overlaps(out[i].p, out[i].bytes, r.p, r.bytes)) return FA_ERR_ALIAS;
+        }
+        for (int j = 0; j < i; ++j)
+            if (overlaps(out[i].p, out[i].bytes, out[j].p, out[j].bytes)) return FA_ERR_ALIAS;
+    }
+    return FA_OK;
+}
+
 }  // namespace fa

@@ -27,12 +27,28 @@ struct Problem {
     int page_size, max_pages, num_pages;
 };
 
+// New keys and values into a cache, with the rotation by positions (fa_kvcache_append).
+struct AppendProblem {
+    const void *k, *v;            // [B][N][Hkv][D], k_stride / v_stride elements between tokens
+    void *k_cache, *v_cache;      // [B][Nk][Hkv][D], or pools of pages
+    const void *q;                // [B][N][Hq][D], q_stride elements between tokens, or NULL
+    void *q_out;                  // [B][N][Hq][D] dense
+    const int *seqlens;
+    int B, Hq, Hkv, N, Nk, D;
+    long long q_stride, k_stride, v_stride;
+    const fa_rotary_t *rotary;    // NULL: no rotation
+    fa_dtype_t dtype;
+    const int *block_table;       // paged: as in Problem
+    int page_size, max_pages, num_pages;
+};
+
 // Each launcher enqueues its kernels on `stream` and returns the first HIP
 // error (hipSuccess when the launch was accepted).
 hipError_t launch_prefill(const Problem &p, hipStream_t stream);
 hipError_t launch_generic(const Problem &p, hipStream_t stream);
 hipError_t launch_decode(const Problem &p, int splits, void *workspace, hipStream_t stream);
 hipError_t launch_unfused(const Problem &p, void *workspace, hipStream_t stream);
+hipError_t launch_append(const AppendProblem &p, hipStream_t stream);
 hipError_t launch_q8_gemv(const void *w, const void *x, void *y, int M, int K, fa_dtype_t x_dtype,
                           fa_dtype_t y_dtype, hipStream_t stream);
 
