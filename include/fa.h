@@ -90,7 +90,8 @@ typedef enum FA_ENUM_BASE {
     FA_ERR_HIP = 11,         /* a HIP runtime call or kernel launch failed */
     FA_ERR_SPLITS = 12,      /* num_splits outside [0, FA_MAX_SPLITS] */
     FA_ERR_PACKING = 13,     /* slots or heads per workgroup not allowed (see fa_fwd_slots) */
-    FA_ERR_ROTARY = 14       /* rotary description not allowed (see fa_rotary_t) */
+    FA_ERR_ROTARY = 14,      /* rotary description not allowed (see fa_rotary_t) */
+    FA_ERR_WINDOW = 15       /* window < 1 or sinks < 0 (see fa_fwd_window) */
 } fa_status_t;
 
 #define FA_MAX_SPLITS 256
@@ -435,6 +436,47 @@ fa_status_t fa_kvcache_append_paged(const void *k, const void *v, void *k_pages,
                                     int page_size, int max_pages, int num_pages,
                                     long long q_stride, long long k_stride, long long v_stride,
                                     const fa_rotary_t *rotary, void *stream, fa_dtype_t dtype);
+
+/* Causal attention with a sliding window and first tokens that stay visible
+ * ("sinks"): the query at position p sees key j iff
+ *   j <= p  and  (j > p - window  or  j < sinks),
+ * that is the `window` keys up to and with its own, and the first `sinks` keys.
+ * Otherwise the tensors and the result are those of fa_fwd_kvcache with causal =
+ * 1: the Nq queries are the last Nq positions of their sequence (p = i +
+ * seqlens_k[b] - Nq), a row that sees no key (seqlens_k[b] < Nq) gives 0 and -inf,
+ * the types and head sizes are fa_fwd's.  seqlens_k may be NULL: Nk keys each.
+ * Any window >= 1 and sinks >= 0 (more than there are keys: all of them).
+ * Only tiles that hold a visible key are read.  Keys that no query of the
+ * call's sequence sees (between the sinks and the first query's window, or past
+ * the length) may hold anything, also infinities and NaN; keys that some do see
+ * must be finite, since a weight of 0 times an infinite value is NaN.
+ * workspace, workspace_bytes: this call's own decode workspace
+ * (fa_window_workspace_bytes; used with Nq = 1 as fa_fwd_ws does), or NULL and 0:
+ * the library's or the one that is set.  Graphs that may run at the same time
+ * need workspaces of their own.
+ * Errors: FA_ERR_WINDOW for window < 1 or sinks < 0; otherwise those of
+ * fa_fwd_kvcache_ws (of fa_fwd_kvcache without a workspace). */
+fa_status_t fa_fwd_window(const void *q, const void *k, const void *v, void *o, float *lse,
+                          const int *seqlens_k, int B, int Hq, int Hkv, int Nq, int Nk, int D,
+                          int window, int sinks, float scale, void *stream, fa_dtype_t in_dtype,
+                          fa_dtype_t out_dtype, void *workspace, size_t workspace_bytes);
+
+/* fa_fwd_window against the paged cache of fa_fwd_kvcache_paged (its types and
+ * head sizes).  Table entries of pages that hold no visible key of the sequence
+ * are not used: they may name pages that belong to others by now.  Errors:
+ * FA_ERR_WINDOW; otherwise those of fa_fwd_kvcache_paged_ws. */
+fa_status_t fa_fwd_window_paged(const void *q, const void *k_pages, const void *v_pages, void *o,
+                                float *lse, const int *seqlens_k, const int *block_table, int B,
+                                int Hq, int Hkv, int Nq, int D, int page_size, int max_pages,
+                                int num_pages, int window, int sinks, float scale, void *stream,
+                                fa_dtype_t in_dtype, fa_dtype_t out_dtype, void *workspace,
+                                size_t workspace_bytes);
+
+/* Bytes of decode workspace that fa_fwd_window (Nk = page_size * max_pages for
+ * the paged form) needs: 0 when the call takes no split-KV path.  The size
+ * serves shorter caches as well. */
+size_t fa_window_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Nk, int D, int window,
+                                 int sinks, fa_dtype_t in_dtype);
 
 #ifdef __cplusplus
 }

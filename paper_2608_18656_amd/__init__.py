@@ -13,7 +13,8 @@ from . import _lib
 
 __all__ = ["fwd", "fwd_splitkv", "fwd_splitkv_noalloc", "fwd_kvcache", "fwd_kvcache_paged", "fwd_unfused",
            "unfused_workspace_bytes", "q8_0_gemv", "FaError", "validate", "workspace_bytes", "release_workspace",
-           "set_workspace", "version", "DTYPE_CODES", "kvcache_append", "kvcache_append_paged"]
+           "set_workspace", "version", "DTYPE_CODES", "kvcache_append", "kvcache_append_paged",
+           "fwd_window", "fwd_window_paged", "window_workspace_bytes"]
 
 
 class FaError(RuntimeError):
@@ -212,6 +213,12 @@ def fwd_unfused(q, k, v, causal: bool = False, scale: float | None = None, out=N
     return out, lse
 
 
+def _check_lengths(rt, seqlens_k, B, device):
+    if (seqlens_k.dtype != rt.int32 or seqlens_k.shape != (B,) or not seqlens_k.is_contiguous()
+            or seqlens_k.device != device):
+        raise ValueError("seqlens_k must be a contiguous int32 [B] tensor on q's device")
+
+
 def fwd_kvcache(q, k_cache, v_cache, seqlens_k, causal: bool = False, scale: float | None = None,
                 out=None, lse=None, out_dtype=None, return_lse: bool = True, workspace=None):
     """Attention against K/V caches [B, Nk, Hkv, D] of which the first
@@ -224,9 +231,7 @@ def fwd_kvcache(q, k_cache, v_cache, seqlens_k, causal: bool = False, scale: flo
     rt = _runtime()
     (B, Hq, Hkv, Nq, Nk, D), out, lse, odt = _prepare(rt, q, k_cache, v_cache, out, lse, out_dtype,
                                                       return_lse)
-    if (not seqlens_k.is_cuda or seqlens_k.dtype != rt.int32 or tuple(seqlens_k.shape) != (B,)
-            or not seqlens_k.is_contiguous() or seqlens_k.device != q.device):
-        raise ValueError("seqlens_k must be a contiguous int32 [B] tensor on q's device")
+    _check_lengths(rt, seqlens_k, B, q.device)
     if scale is None:
         scale = 1.0 / math.sqrt(D)
     index = q.device.index
@@ -241,18 +246,9 @@ def fwd_kvcache(q, k_cache, v_cache, seqlens_k, causal: bool = False, scale: flo
     return out, lse
 
 
-def fwd_kvcache_paged(q, k_pages, v_pages, block_table, seqlens_k, causal: bool = False,
-                      scale: float | None = None, out=None, lse=None, out_dtype=None,
-                      return_lse: bool = True, workspace=None):
-    """Attention against a paged K/V cache: ``k_pages``, ``v_pages``
-    [num_pages, page_size, Hkv, D] (page_size a multiple of 64), ``block_table``
-    int32 [B, max_pages] (page of each block of page_size keys of each
-    sequence), ``seqlens_k`` int32 [B]; q [B, Nq, Hq, D] holds each sequence's
-    last Nq positions.  ``workspace``: this call's own decode workspace
-    (uint8 GPU tensor; fa_fwd_kvcache_paged_ws).  See fa_fwd_kvcache_paged in
-    include/fa.h."""
-    lib = _lib.load()
-    rt = _runtime()
+def _prepare_paged(rt, q, k_pages, v_pages, block_table, seqlens_k, out, lse, out_dtype, return_lse):
+    """As ``_prepare`` for a paged cache; the sizes are B, Hq, Hkv, Nq, D,
+    page_size, max_pages, num_pages."""
     for name, t in (("q", q), ("k_pages", k_pages), ("v_pages", v_pages)):
         if not t.is_cuda or not t.is_contiguous() or t.dim() != 4:
             raise ValueError(f"{name} must be a contiguous 4-D GPU tensor")
@@ -273,21 +269,91 @@ def fwd_kvcache_paged(q, k_pages, v_pages, block_table, seqlens_k, causal: bool 
             raise ValueError(f"{name} must be a contiguous int32 tensor on q's device")
     if block_table.dim() != 2 or block_table.shape[0] != B:
         raise ValueError("block_table must be [B, max_pages]")
-    max_pages = block_table.shape[1]
     odt = dt if out_dtype is None else out_dtype
     out, lse = _outputs(rt, q, out, lse, odt, return_lse, B, Hq, Nq)
+    return (B, Hq, Hkv, Nq, D, page_size, block_table.shape[1], num_pages), out, lse, odt
+
+
+def fwd_kvcache_paged(q, k_pages, v_pages, block_table, seqlens_k, causal: bool = False,
+                      scale: float | None = None, out=None, lse=None, out_dtype=None,
+                      return_lse: bool = True, workspace=None):
+    """Attention against a paged K/V cache: ``k_pages``, ``v_pages``
+    [num_pages, page_size, Hkv, D] (page_size a multiple of 64), ``block_table``
+    int32 [B, max_pages] (page of each block of page_size keys of each
+    sequence), ``seqlens_k`` int32 [B]; q [B, Nq, Hq, D] holds each sequence's
+    last Nq positions.  ``workspace``: this call's own decode workspace
+    (uint8 GPU tensor; fa_fwd_kvcache_paged_ws).  See fa_fwd_kvcache_paged in
+    include/fa.h."""
+    lib = _lib.load()
+    rt = _runtime()
+    dims, out, lse, odt = _prepare_paged(rt, q, k_pages, v_pages, block_table, seqlens_k, out, lse, out_dtype, return_lse)
     if scale is None:
-        scale = 1.0 / math.sqrt(D)
-    index = dev.index
+        scale = 1.0 / math.sqrt(dims[4])
+    index = q.device.index
     args = (q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), out.data_ptr(),
             lse.data_ptr() if lse is not None else None, seqlens_k.data_ptr(), block_table.data_ptr(),
-            B, Hq, Hkv, Nq, D, page_size, max_pages, num_pages, 1 if causal else 0, float(scale),
-            rt.stream(index), rt.codes[dt], rt.codes.get(odt, -1))
+            *dims, 1 if causal else 0, float(scale), rt.stream(index), rt.codes[q.dtype], rt.codes.get(odt, -1))
     if workspace is not None:
-        _call(rt, lib, index, lib.fa_fwd_kvcache_paged_ws, (*args, *_workspace_arg(workspace, dev)))
+        _call(rt, lib, index, lib.fa_fwd_kvcache_paged_ws, (*args, *_workspace_arg(workspace, q.device)))
     else:
         _call(rt, lib, index, lib.fa_fwd_kvcache_paged, args)
     return out, lse
+
+
+def window_workspace_bytes(B, Hq, Hkv, Nq, Nk, D, window, in_dtype: str, sinks: int = 0) -> int:
+    """Decode workspace bytes of fwd_window (fa_window_workspace_bytes)."""
+    return int(_lib.load().fa_window_workspace_bytes(B, Hq, Hkv, Nq, Nk, D, _int32(window), _int32(sinks),
+                                                     DTYPE_CODES[in_dtype]))
+
+
+def fwd_window(q, k, v, window: int, sinks: int = 0, seqlens_k=None, scale: float | None = None, out=None, lse=None,
+               out_dtype=None, return_lse: bool = True, workspace=None):
+    """Causal attention with a sliding window: the query at position p sees the
+    ``window`` keys p - window + 1 .. p and the first ``sinks`` keys
+    (fa_fwd_window).  q [B, Nq, Hq, D] holds the last Nq of each sequence's
+    ``seqlens_k`` (int32 [B]; None: Nk) keys in k, v [B, Nk, Hkv, D]: a whole
+    prompt, a chunk of one, or one token.  Rows that see no key give 0 and lse
+    -inf.  ``workspace``: this call's own decode workspace (uint8 GPU tensor of
+    window_workspace_bytes(...) bytes).  Returns (out, lse) as ``fwd``."""
+    lib = _lib.load()
+    rt = _runtime()
+    dims, out, lse, odt = _prepare(rt, q, k, v, out, lse, out_dtype, return_lse)
+    if seqlens_k is not None:
+        _check_lengths(rt, seqlens_k, dims[0], q.device)
+    if scale is None:
+        scale = 1.0 / math.sqrt(dims[5])
+    index = q.device.index
+    _call(rt, lib, index, lib.fa_fwd_window,
+          (q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else None,
+           seqlens_k.data_ptr() if seqlens_k is not None else None, *dims, _int32(window), _int32(sinks), float(scale),
+           rt.stream(index), rt.codes[q.dtype], rt.codes.get(odt, -1),
+           *((None, 0) if workspace is None else _workspace_arg(workspace, q.device))))
+    return out, lse
+
+
+def fwd_window_paged(q, k_pages, v_pages, block_table, seqlens_k, window: int, sinks: int = 0,
+                     scale: float | None = None, out=None, lse=None, out_dtype=None, return_lse: bool = True,
+                     workspace=None):
+    """``fwd_window`` against the paged cache of ``fwd_kvcache_paged``.  Pages
+    that hold no visible key are not read (fa_fwd_window_paged)."""
+    lib = _lib.load()
+    rt = _runtime()
+    dims, out, lse, odt = _prepare_paged(rt, q, k_pages, v_pages, block_table, seqlens_k, out, lse, out_dtype, return_lse)
+    if scale is None:
+        scale = 1.0 / math.sqrt(dims[4])
+    index = q.device.index
+    _call(rt, lib, index, lib.fa_fwd_window_paged,
+          (q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), out.data_ptr(),
+           lse.data_ptr() if lse is not None else None, seqlens_k.data_ptr(), block_table.data_ptr(), *dims,
+           _int32(window), _int32(sinks), float(scale), rt.stream(index), rt.codes[q.dtype], rt.codes.get(odt, -1),
+           *((None, 0) if workspace is None else _workspace_arg(workspace, q.device))))
+    return out, lse
+
+
+def _int32(n):
+    """n, at most what a C int holds (a window past every cache is like any other), and
+    at least -1 (refused like any negative number)."""
+    return max(min(int(n), 0x7fffffff), -1)
 
 
 def _token_stride(t, name):

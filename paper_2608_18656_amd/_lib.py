@@ -19,7 +19,7 @@ STATUS_NAMES = {
     0: "FA_OK", 1: "FA_ERR_NULL", 2: "FA_ERR_DIM", 3: "FA_ERR_GQA_RATIO", 4: "FA_ERR_HEAD_DIM",
     5: "FA_ERR_CAUSAL_SHAPE", 6: "FA_ERR_SCALE", 7: "FA_ERR_ALIGN", 8: "FA_ERR_ALIAS",
     9: "FA_ERR_DTYPE", 10: "FA_ERR_WORKSPACE", 11: "FA_ERR_HIP", 12: "FA_ERR_SPLITS",
-    13: "FA_ERR_PACKING", 14: "FA_ERR_ROTARY",
+    13: "FA_ERR_PACKING", 14: "FA_ERR_ROTARY", 15: "FA_ERR_WINDOW",
 }
 
 # Every symbol include/fa.h declares.
@@ -28,7 +28,8 @@ EXPORTS = ("fa_status_string", "fa_version", "fa_validate", "fa_fwd_f16", "fa_fw
            "fa_release_workspace", "fa_set_workspace", "fa_fwd_packed", "fa_fwd_kvcache",
            "fa_q8_0_gemv", "fa_fwd_kvcache_paged", "fa_fwd_unfused", "fa_unfused_workspace_bytes",
            "fa_fwd_ws", "fa_fwd_kvcache_ws", "fa_fwd_kvcache_paged_ws", "fa_fwd_splitkv_noalloc", "fa_fwd_slots",
-           "fa_kvcache_append", "fa_kvcache_append_paged")
+           "fa_kvcache_append", "fa_kvcache_append_paged", "fa_fwd_window", "fa_fwd_window_paged",
+           "fa_window_workspace_bytes")
 
 _lib = None
 
@@ -105,5 +106,11 @@ def load():
     lib.fa_kvcache_append.restype = _I
     lib.fa_kvcache_append_paged.argtypes = [_P] * 8 + [_I] * 8 + [_L] * 3 + [_P, _P, _I]
     lib.fa_kvcache_append_paged.restype = _I
+    lib.fa_fwd_window.argtypes = [_P] * 6 + [_I] * 8 + [_F, _P, _I, _I, _P, ctypes.c_size_t]
+    lib.fa_fwd_window.restype = _I
+    lib.fa_fwd_window_paged.argtypes = [_P] * 7 + [_I] * 10 + [_F, _P, _I, _I, _P, ctypes.c_size_t]
+    lib.fa_fwd_window_paged.restype = _I
+    lib.fa_window_workspace_bytes.argtypes = [_I] * 9
+    lib.fa_window_workspace_bytes.restype = ctypes.c_size_t
     _lib = lib
     return lib

@@ -40,6 +40,7 @@ def hipcc() -> str:
 PER_FILE_FLAGS = {
     "fa_prefill.hip": ["-fno-honor-nans"],
     "fa_decode.hip": ["-fno-honor-nans"],
+    "fa_window.hip": ["-fno-honor-nans"],
 }
 
 

@@ -120,6 +120,17 @@ fa_status_t scratch_address(void **out) {
     return FA_OK;
 }
 
+// What a query sees, besides causal: with size > 0 the `size` keys up to its own and the first `sinks`.
+struct Window {
+    int size = 0, sinks = 0;
+};
+
+// Keys that a decode call with this window reads, at most.
+int decode_keys(int Nk, const Window &w) {
+    const long long n = (long long)w.size + w.sinks;
+    return w.size > 0 && n < Nk ? (int)n : Nk;
+}
+
 struct Paging {
     const int *block_table = nullptr;
     int page_size = 0, max_pages = 0, num_pages = 0;
@@ -129,7 +140,7 @@ fa_status_t run(const void *q, const void *k, const void *v, void *o, float *lse
                 int Hkv, int Nq, int Nk, int D, int causal, float scale, void *stream,
                 fa_dtype_t in, fa_dtype_t out, int splits_req, int hw_req = 0,
                 const int *seqlens = nullptr, const Paging &pg = Paging(),
-                const CallWs *cws = nullptr, int slots_req = 0) {
+                const CallWs *cws = nullptr, int slots_req = 0, const Window &win = Window()) {
     const long long kv_rows = pg.block_table ? (long long)pg.num_pages * pg.page_size : -1;
     fa_status_t st = validate_core(q, k, v, o, lse, B, Hq, Hkv, Nq, Nk, D, causal, scale, in, out, kv_rows);
     if (st != FA_OK) return st;
@@ -140,11 +151,13 @@ fa_status_t run(const void *q, const void *k, const void *v, void *o, float *lse
         (hw_req > 0 && ((Hq / Hkv) % hw_req != 0 || slots % hw_req != 0)))
         return FA_ERR_PACKING;
     fa::Problem p{q, k, v, o, lse, B, Hq, Hkv, Nq, Nk, D, causal, scale, in, out, hw_req, slots_req, seqlens,
-                  pg.block_table, pg.page_size, pg.max_pages, pg.num_pages};
+                  pg.block_table, pg.page_size, pg.max_pages, pg.num_pages,
+                  win.size < Nk ? win.size : Nk, win.sinks < Nk ? win.sinks : Nk};
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     hipError_t e;
     if (fa::decode_supported(Nq, Hkv, D, in)) {
-        const int S = splits_req > 0 ? splits_req : fa::decode_default_splits(B, Hq, Hkv, Nk, D);
+        const int keys = decode_keys(Nk, win);
+        const int S = splits_req > 0 ? splits_req : fa::decode_default_splits(B, Hq, Hkv, keys, D);
         const size_t need = fa::decode_workspace_bytes(B, Hq, D, S);
         void *ws = nullptr;
         bool user = false;
@@ -155,7 +168,7 @@ fa_status_t run(const void *q, const void *k, const void *v, void *o, float *lse
             ws = cws->ptr;
             user = true;
         } else {
-            const int most = splits_req > 0 ? splits_req : fa::decode_most_splits(B, Hq, Hkv, Nk, D);
+            const int most = splits_req > 0 ? splits_req : fa::decode_most_splits(B, Hq, Hkv, keys, D);
             st = get_workspace(need, fa::decode_workspace_bytes(B, Hq, D, most), s, &ws, &user);
             if (st != FA_OK) return st;
         }
@@ -169,9 +182,9 @@ fa_status_t run(const void *q, const void *k, const void *v, void *o, float *lse
         }
         e = fa::launch_decode(p, S, ws, s);
     } else if (fa::prefill_supported(Hkv, D, in)) {
-        e = fa::launch_prefill(p, s);
+        e = win.size > 0 ? fa::launch_prefill_window(p, s) : fa::launch_prefill(p, s);
     } else {
-        e = fa::launch_generic(p, s);
+        e = win.size > 0 ? fa::launch_generic_window(p, s) : fa::launch_generic(p, s);
     }
     return e == hipSuccess ? FA_OK : FA_ERR_HIP;
 }
@@ -202,6 +215,7 @@ const char *fa_status_string(fa_status_t s) {
     case FA_ERR_ROTARY:
         return "FA_ERR_ROTARY: rot_dim must be even, 2 to D; axes 1 to 4, with positions if several, and pair_axis "
                "below axes";
+    case FA_ERR_WINDOW: return "FA_ERR_WINDOW: window must be at least 1 and sinks not negative";
     }
     return "unknown fa_status_t";
 }
@@ -263,7 +277,7 @@ namespace {
 fa_status_t kvcache(const void *q, const void *k, const void *v, void *o, float *lse,
                     const int *seqlens_k, int B, int Hq, int Hkv, int Nq, int Nk, int D, int causal,
                     float scale, void *stream, fa_dtype_t in_dtype, fa_dtype_t out_dtype,
-                    const CallWs *cws) {
+                    const CallWs *cws, const Window &win = Window()) {
     if (!seqlens_k) return FA_ERR_NULL;
     if (reinterpret_cast<uintptr_t>(seqlens_k) & 3) return FA_ERR_ALIGN;
     if (B >= 1 && o && Hq >= 1 && Nq >= 1 && D >= 1) {
@@ -273,7 +287,7 @@ fa_status_t kvcache(const void *q, const void *k, const void *v, void *o, float 
             return FA_ERR_ALIAS;
     }
     return run(q, k, v, o, lse, B, Hq, Hkv, Nq, Nk, D, causal, scale, stream, in_dtype, out_dtype, 0,
-               0, seqlens_k, Paging(), cws);
+               0, seqlens_k, Paging(), cws, 0, win);
 }
 
 bool pages_ok(int B, int page_size, int max_pages, int num_pages) {
@@ -300,7 +314,7 @@ fa_status_t kvcache_paged(const void *q, const void *k_pages, const void *v_page
                           float *lse, const int *seqlens_k, const int *block_table, int B, int Hq,
                           int Hkv, int Nq, int D, int page_size, int max_pages, int num_pages,
                           int causal, float scale, void *stream, fa_dtype_t in_dtype,
-                          fa_dtype_t out_dtype, const CallWs *cws) {
+                          fa_dtype_t out_dtype, const CallWs *cws, const Window &win = Window()) {
     if (!seqlens_k || !block_table) return FA_ERR_NULL;
     if (!pages_ok(B, page_size, max_pages, num_pages)) return FA_ERR_DIM;
     if ((reinterpret_cast<uintptr_t>(seqlens_k) & 3) || (reinterpret_cast<uintptr_t>(block_table) & 3))
@@ -331,7 +345,7 @@ fa_status_t kvcache_paged(const void *q, const void *k_pages, const void *v_page
     pg.max_pages = max_pages;
     pg.num_pages = num_pages;
     return run(q, k_pages, v_pages, o, lse, B, Hq, Hkv, Nq, Nk, D, causal, scale, stream, in_dtype,
-               out_dtype, 0, 0, seqlens_k, pg, cws);
+               out_dtype, 0, 0, seqlens_k, pg, cws, 0, win);
 }
 
 }  // namespace
@@ -453,6 +467,38 @@ fa_status_t fa_q8_0_gemv(const void *w, const void *x, void *y, int M, int K, fa
     const hipError_t e =
         fa::launch_q8_gemv(w, x, y, M, K, x_dtype, y_dtype, reinterpret_cast<hipStream_t>(stream));
     return e == hipSuccess ? FA_OK : FA_ERR_HIP;
+}
+
+fa_status_t fa_fwd_window(const void *q, const void *k, const void *v, void *o, float *lse, const int *seqlens_k,
+                          int B, int Hq, int Hkv, int Nq, int Nk, int D, int window, int sinks, float scale,
+                          void *stream, fa_dtype_t in_dtype, fa_dtype_t out_dtype, void *workspace,
+                          size_t workspace_bytes) {
+    if (window < 1 || sinks < 0) return FA_ERR_WINDOW;
+    const CallWs cws{workspace, workspace_bytes}, *own = workspace || workspace_bytes ? &cws : nullptr;
+    const Window win{window, sinks};
+    if (seqlens_k)
+        return kvcache(q, k, v, o, lse, seqlens_k, B, Hq, Hkv, Nq, Nk, D, 1, scale, stream, in_dtype, out_dtype, own,
+                       win);
+    return run(q, k, v, o, lse, B, Hq, Hkv, Nq, Nk, D, 1, scale, stream, in_dtype, out_dtype, 0, 0, nullptr, Paging(),
+               own, 0, win);
+}
+
+fa_status_t fa_fwd_window_paged(const void *q, const void *k_pages, const void *v_pages, void *o, float *lse,
+                                const int *seqlens_k, const int *block_table, int B, int Hq, int Hkv, int Nq, int D,
+                                int page_size, int max_pages, int num_pages, int window, int sinks, float scale,
+                                void *stream, fa_dtype_t in_dtype, fa_dtype_t out_dtype, void *workspace,
+                                size_t workspace_bytes) {
+    if (window < 1 || sinks < 0) return FA_ERR_WINDOW;
+    const CallWs cws{workspace, workspace_bytes};
+    return kvcache_paged(q, k_pages, v_pages, o, lse, seqlens_k, block_table, B, Hq, Hkv, Nq, D, page_size, max_pages,
+                         num_pages, 1, scale, stream, in_dtype, out_dtype,
+                         workspace || workspace_bytes ? &cws : nullptr, Window{window, sinks});
+}
+
+size_t fa_window_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Nk, int D, int window, int sinks,
+                                 fa_dtype_t in_dtype) {
+    if (window < 1 || sinks < 0 || Nk < 1) return 0;
+    return fa_workspace_bytes(B, Hq, Hkv, Nq, decode_keys(Nk, Window{window, sinks}), D, in_dtype, 0);
 }
 
 fa_status_t fa_kvcache_append(const void *k, const void *v, void *k_cache, void *v_cache, const void *q,

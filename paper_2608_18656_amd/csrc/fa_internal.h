@@ -25,6 +25,9 @@ struct Problem {
     // block_table[b * max_pages + j / page_size]; Nk = page_size * max_pages.
     const int *block_table;
     int page_size, max_pages, num_pages;
+    // window > 0: a query sees the window keys up to its own position and the
+    // first `sinks` (causal is set; both at most Nk)
+    int window = 0, sinks = 0;
 };
 
 // New keys and values into a cache, with the rotation by positions (fa_kvcache_append).
@@ -45,7 +48,9 @@ struct AppendProblem {
 // Each launcher enqueues its kernels on `stream` and returns the first HIP
 // error (hipSuccess when the launch was accepted).
 hipError_t launch_prefill(const Problem &p, hipStream_t stream);
+hipError_t launch_prefill_window(const Problem &p, hipStream_t stream);
 hipError_t launch_generic(const Problem &p, hipStream_t stream);
+hipError_t launch_generic_window(const Problem &p, hipStream_t stream);
 hipError_t launch_decode(const Problem &p, int splits, void *workspace, hipStream_t stream);
 hipError_t launch_unfused(const Problem &p, void *workspace, hipStream_t stream);
 hipError_t launch_append(const AppendProblem &p, hipStream_t stream);
