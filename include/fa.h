@@ -478,6 +478,52 @@ fa_status_t fa_fwd_window_paged(const void *q, const void *k_pages, const void *
 size_t fa_window_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Nk, int D, int window,
                                  int sinks, fa_dtype_t in_dtype);
 
+/* Attention of a batch whose sequences begin with the same Np keys (one system
+ * prompt and many conversations, many answers to one question): the result of
+ * fa_fwd_kvcache on each sequence's prefix and suffix one after the other, with
+ * the prefix read for all sequences together instead of once for each.
+ *   k_prefix, v_prefix  [Np][Hkv][D]      the shared keys and values
+ *   k, v                [B][Nk][Hkv][D]   each sequence's own, of which the first
+ *                       seqlens_k[b] are valid (int32, device; NULL: Nk each)
+ * The Nq queries of sequence b are the last Nq of its Np + seqlens_k[b] positions;
+ * with causal = 1 query i sees its first i + 1 + Np + seqlens_k[b] - Nq keys (a row
+ * that sees none gives 0 and -inf).  fp16 / bf16 with D in {64, 128}.
+ * workspace, workspace_bytes: device scratch of this call
+ * (fa_prefix_workspace_bytes), 16-byte aligned, or NULL and 0: the library's or
+ * the one that is set (see the top).  Graphs that may run at the same time need
+ * workspaces of their own.
+ * Errors: FA_ERR_NULL for a NULL tensor (or workspace with a size), FA_ERR_DIM
+ * for a size < 1, Np + Nk above FA_MAX_PREFIX_KEYS, B * Nq * Hq above 2^31 - 1 or
+ * key rows above 33 MiB, FA_ERR_DTYPE for fp32 inputs, FA_ERR_HEAD_DIM for another
+ * D, FA_ERR_CAUSAL_SHAPE for causal with Nq > Np + Nk, FA_ERR_WORKSPACE for a
+ * workspace too small; otherwise as fa_fwd_kvcache. */
+#define FA_MAX_PREFIX_KEYS (1 << 30)
+fa_status_t fa_fwd_prefix(const void *q, const void *k_prefix, const void *v_prefix, const void *k,
+                          const void *v, void *o, float *lse, const int *seqlens_k, int B, int Hq,
+                          int Hkv, int Nq, int Np, int Nk, int D, int causal, float scale,
+                          void *stream, fa_dtype_t in_dtype, fa_dtype_t out_dtype, void *workspace,
+                          size_t workspace_bytes);
+
+/* fa_fwd_prefix against the paged cache of fa_fwd_kvcache_paged, the arguments
+ * and the result of that call (lengths count the prefix; a sequence may be
+ * shorter than it): the first prefix_len keys of all sequences are in the same
+ * pages, those that the first row of the table names; the other rows' entries
+ * for them are not read.  prefix_len: a positive multiple of page_size, at most
+ * page_size * max_pages.  Workspace: fa_prefix_workspace_bytes with Np =
+ * prefix_len, Nk = page_size * max_pages - prefix_len.  Errors: FA_ERR_DIM for
+ * another prefix_len; otherwise those of fa_fwd_prefix and fa_fwd_kvcache_paged. */
+fa_status_t fa_fwd_prefix_paged(const void *q, const void *k_pages, const void *v_pages, void *o,
+                                float *lse, const int *seqlens_k, const int *block_table, int B,
+                                int Hq, int Hkv, int Nq, int D, int page_size, int max_pages,
+                                int num_pages, int prefix_len, int causal, float scale,
+                                void *stream, fa_dtype_t in_dtype, fa_dtype_t out_dtype,
+                                void *workspace, size_t workspace_bytes);
+
+/* Bytes of workspace that fa_fwd_prefix needs (0 for sizes it refuses); serves
+ * every shorter prefix and suffix as well. */
+size_t fa_prefix_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Np, int Nk, int D,
+                                 fa_dtype_t in_dtype);
+
 #ifdef __cplusplus
 }
 #endif

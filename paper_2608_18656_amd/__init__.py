@@ -14,7 +14,8 @@ from . import _lib
 __all__ = ["fwd", "fwd_splitkv", "fwd_splitkv_noalloc", "fwd_kvcache", "fwd_kvcache_paged", "fwd_unfused",
            "unfused_workspace_bytes", "q8_0_gemv", "FaError", "validate", "workspace_bytes", "release_workspace",
            "set_workspace", "version", "DTYPE_CODES", "kvcache_append", "kvcache_append_paged",
-           "fwd_window", "fwd_window_paged", "window_workspace_bytes"]
+           "fwd_window", "fwd_window_paged", "window_workspace_bytes", "fwd_prefix", "fwd_prefix_paged",
+           "prefix_workspace_bytes"]
 
 
 class FaError(RuntimeError):
@@ -347,6 +348,62 @@ def fwd_window_paged(q, k_pages, v_pages, block_table, seqlens_k, window: int, s
            lse.data_ptr() if lse is not None else None, seqlens_k.data_ptr(), block_table.data_ptr(), *dims,
            _int32(window), _int32(sinks), float(scale), rt.stream(index), rt.codes[q.dtype], rt.codes.get(odt, -1),
            *((None, 0) if workspace is None else _workspace_arg(workspace, q.device))))
+    return out, lse
+
+
+def prefix_workspace_bytes(B, Hq, Hkv, Nq, Np, Nk, D, in_dtype: str) -> int:
+    """Workspace bytes of fwd_prefix (fa_prefix_workspace_bytes)."""
+    return int(_lib.load().fa_prefix_workspace_bytes(B, Hq, Hkv, Nq, Np, Nk, D, DTYPE_CODES[in_dtype]))
+
+
+def fwd_prefix(q, k_prefix, v_prefix, k, v, seqlens_k=None, causal: bool = False, scale: float | None = None,
+               out=None, lse=None, out_dtype=None, return_lse: bool = True, workspace=None):
+    """Attention of a batch whose sequences share a prefix, which is read once
+    for all of them: ``fwd_kvcache`` on each sequence's prefix and suffix one
+    after the other (fa_fwd_prefix).  ``k_prefix``, ``v_prefix`` [Np, Hkv, D]; ``k``,
+    ``v`` [B, Nk, Hkv, D], each sequence's own keys, of which the first
+    ``seqlens_k`` (int32 [B]; None: Nk) are valid; q [B, Nq, Hq, D] holds the last
+    Nq positions of each.  fp16 / bf16, D in {64, 128}.  ``workspace``: this call's
+    own scratch (uint8 GPU tensor of prefix_workspace_bytes(...) bytes).  Returns
+    (out, lse) as ``fwd``."""
+    lib = _lib.load()
+    rt = _runtime()
+    (B, Hq, Hkv, Nq, Nk, D), out, lse, odt = _prepare(rt, q, k, v, out, lse, out_dtype, return_lse)
+    if (k_prefix.dim() != 3 or k_prefix.shape != v_prefix.shape or k_prefix.shape[1:] != k.shape[2:]
+            or not k_prefix.is_contiguous() or not v_prefix.is_contiguous() or k_prefix.dtype != q.dtype
+            or v_prefix.dtype != q.dtype or k_prefix.device != q.device or v_prefix.device != q.device):
+        raise ValueError("k_prefix and v_prefix must be contiguous [Np, Hkv, D] tensors of q's dtype and device")
+    if seqlens_k is not None:
+        _check_lengths(rt, seqlens_k, B, q.device)
+    if scale is None:
+        scale = 1.0 / math.sqrt(D)
+    index = q.device.index
+    _call(rt, lib, index, lib.fa_fwd_prefix,
+          (q.data_ptr(), k_prefix.data_ptr(), v_prefix.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+           lse.data_ptr() if lse is not None else None, seqlens_k.data_ptr() if seqlens_k is not None else None,
+           B, Hq, Hkv, Nq, k_prefix.shape[0], Nk, D, 1 if causal else 0, float(scale), rt.stream(index),
+           rt.codes[q.dtype], rt.codes.get(odt, -1),
+           *((None, 0) if workspace is None else _workspace_arg(workspace, q.device))))
+    return out, lse
+
+
+def fwd_prefix_paged(q, k_pages, v_pages, block_table, seqlens_k, prefix_len: int, causal: bool = False,
+                     scale: float | None = None, out=None, lse=None, out_dtype=None, return_lse: bool = True,
+                     workspace=None):
+    """``fwd_kvcache_paged`` for sequences whose first ``prefix_len`` keys (a
+    multiple of the page size) lie in the same pages, those of ``block_table[0]``:
+    these are read once for the whole batch (fa_fwd_prefix_paged)."""
+    lib = _lib.load()
+    rt = _runtime()
+    dims, out, lse, odt = _prepare_paged(rt, q, k_pages, v_pages, block_table, seqlens_k, out, lse, out_dtype, return_lse)
+    if scale is None:
+        scale = 1.0 / math.sqrt(dims[4])
+    index = q.device.index
+    _call(rt, lib, index, lib.fa_fwd_prefix_paged,
+          (q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), out.data_ptr(),
+           lse.data_ptr() if lse is not None else None, seqlens_k.data_ptr(), block_table.data_ptr(), *dims,
+           _int32(prefix_len), 1 if causal else 0, float(scale), rt.stream(index), rt.codes[q.dtype],
+           rt.codes.get(odt, -1), *((None, 0) if workspace is None else _workspace_arg(workspace, q.device))))
     return out, lse
 
 

@@ -29,7 +29,7 @@ EXPORTS = ("fa_status_string", "fa_version", "fa_validate", "fa_fwd_f16", "fa_fw
            "fa_q8_0_gemv", "fa_fwd_kvcache_paged", "fa_fwd_unfused", "fa_unfused_workspace_bytes",
            "fa_fwd_ws", "fa_fwd_kvcache_ws", "fa_fwd_kvcache_paged_ws", "fa_fwd_splitkv_noalloc", "fa_fwd_slots",
            "fa_kvcache_append", "fa_kvcache_append_paged", "fa_fwd_window", "fa_fwd_window_paged",
-           "fa_window_workspace_bytes")
+           "fa_window_workspace_bytes", "fa_fwd_prefix", "fa_fwd_prefix_paged", "fa_prefix_workspace_bytes")
 
 _lib = None
 
@@ -112,5 +112,11 @@ def load():
     lib.fa_fwd_window_paged.restype = _I
     lib.fa_window_workspace_bytes.argtypes = [_I] * 9
     lib.fa_window_workspace_bytes.restype = ctypes.c_size_t
+    lib.fa_fwd_prefix.argtypes = [_P] * 8 + [_I] * 8 + [_F, _P, _I, _I, _P, ctypes.c_size_t]
+    lib.fa_fwd_prefix.restype = _I
+    lib.fa_fwd_prefix_paged.argtypes = [_P] * 7 + [_I] * 10 + [_F, _P, _I, _I, _P, ctypes.c_size_t]
+    lib.fa_fwd_prefix_paged.restype = _I
+    lib.fa_prefix_workspace_bytes.argtypes = [_I] * 8
+    lib.fa_prefix_workspace_bytes.restype = ctypes.c_size_t
     _lib = lib
     return lib

@@ -41,6 +41,7 @@ PER_FILE_FLAGS = {
     "fa_prefill.hip": ["-fno-honor-nans"],
     "fa_decode.hip": ["-fno-honor-nans"],
     "fa_window.hip": ["-fno-honor-nans"],
+    "fa_prefix.hip": ["-fno-honor-nans"],
 }
 
 

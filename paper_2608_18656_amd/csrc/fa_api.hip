@@ -310,6 +310,59 @@ fa_status_t append(const void *k, const void *v, void *k_cache, void *v_cache, c
     return fa::launch_append(p, reinterpret_cast<hipStream_t>(stream)) == hipSuccess ? FA_OK : FA_ERR_HIP;
 }
 
+// Attention behind a shared prefix: the checks of both forms, then the launch.
+// table NULL: k, v [B][Nk][Hkv][D] are the suffixes, else the pools, and Nk what a suffix can hold.
+fa_status_t prefix(const void *q, const void *k_prefix, const void *v_prefix, const void *k, const void *v, void *o,
+                   float *lse, const int *seqlens, int B, int Hq, int Hkv, int Nq, int Np, int Nk, int D, int causal,
+                   float scale, void *stream, fa_dtype_t in, fa_dtype_t out, const Paging &pg, void *workspace,
+                   size_t workspace_bytes) {
+    if (!k_prefix || !v_prefix) return FA_ERR_NULL;
+    const bool paged = pg.block_table != nullptr;
+    const long long kv_rows = paged ? (long long)pg.num_pages * pg.page_size : (long long)B * Nk;
+    if (Np < 1 || Nk < (paged ? 0 : 1) || (long long)Np + Nk > FA_MAX_PREFIX_KEYS) return FA_ERR_DIM;
+    const long long tokens = (long long)B * Nq;
+    if (B > 0 && Nq > 0 && Hq > 0 && (tokens > 0x7fffffffLL || tokens * Hq > 0x7fffffffLL)) return FA_ERR_DIM;
+    fa_status_t st = validate_core(q, k, v, o, lse, B, Hq, Hkv, Nq, Nk > 0 ? Nk : 1, D, 0, scale, in, out, kv_rows);
+    if (st != FA_OK) return st;
+    if (in == FA_F32) return FA_ERR_DTYPE;
+    if (D != 64 && D != 128) return FA_ERR_HEAD_DIM;
+    if (causal && Nq > Np + Nk) return FA_ERR_CAUSAL_SHAPE;
+    long long t;
+    if (!fa::mul_ok((long long)Np * Hkv, D, &t) || !fa::prefill_supported(Hkv, D, in)) return FA_ERR_DIM;
+    if (fa::misaligned(k_prefix, 16) || fa::misaligned(v_prefix, 16) || fa::misaligned(seqlens, 4) ||
+        fa::misaligned(pg.block_table, 4))
+        return FA_ERR_ALIGN;
+    const size_t qb = (size_t)B * Nq * Hq * D * esize(in), kb = (size_t)kv_rows * Hkv * D * esize(in);
+    const size_t ob = (size_t)B * Nq * Hq * D * esize(out), lb = (size_t)B * Hq * Nq * sizeof(float);
+    const size_t pb = paged ? kb : (size_t)Np * Hkv * D * esize(in);
+    const fa::Range read[] = {{q, qb}, {k, kb}, {v, kb}, {k_prefix, pb}, {v_prefix, pb},
+                              {seqlens, seqlens ? (size_t)B * sizeof(int) : 0},
+                              {pg.block_table, paged ? (size_t)B * pg.max_pages * sizeof(int) : 0}};
+    for (const fa::Range &r : read)
+        if (r.bytes && (overlaps(o, ob, r.p, r.bytes) || (lse && overlaps(lse, lb, r.p, r.bytes)))) return FA_ERR_ALIAS;
+    const size_t need = fa::prefix_workspace_bytes(B, Hq, Hkv, Nq, Np, Nk, D, false);
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    bool user = workspace || workspace_bytes;
+    if (user) {
+        if (!workspace) return FA_ERR_NULL;
+        if (fa::misaligned(workspace, 16)) return FA_ERR_ALIGN;
+        if (workspace_bytes < need) return FA_ERR_WORKSPACE;
+    } else {
+        st = get_workspace(need, fa::prefix_workspace_bytes(B, Hq, Hkv, Nq, Np, Nk, D, true), s, &workspace, &user);
+        if (st != FA_OK) return st;
+    }
+    if (user) {
+        for (const fa::Range &r : read)
+            if (r.bytes && overlaps(workspace, need, r.p, r.bytes)) return FA_ERR_ALIAS;
+        if (overlaps(workspace, need, o, ob) || (lse && overlaps(workspace, need, lse, lb))) return FA_ERR_ALIAS;
+    }
+    fa::PrefixProblem pp{fa::Problem{q, k, v, o, lse, B, Hq, Hkv, Nq, paged ? pg.page_size * pg.max_pages : Nk, D, causal,
+                                     scale, in, out, 0, 0, seqlens, pg.block_table, pg.page_size, pg.max_pages,
+                                     pg.num_pages},
+                         k_prefix, v_prefix, Np, Nk};
+    return fa::launch_prefix(pp, workspace, s) == hipSuccess ? FA_OK : FA_ERR_HIP;
+}
+
 fa_status_t kvcache_paged(const void *q, const void *k_pages, const void *v_pages, void *o,
                           float *lse, const int *seqlens_k, const int *block_table, int B, int Hq,
                           int Hkv, int Nq, int D, int page_size, int max_pages, int num_pages,
@@ -499,6 +552,40 @@ size_t fa_window_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Nk, int D, 
                                  fa_dtype_t in_dtype) {
     if (window < 1 || sinks < 0 || Nk < 1) return 0;
     return fa_workspace_bytes(B, Hq, Hkv, Nq, decode_keys(Nk, Window{window, sinks}), D, in_dtype, 0);
+}
+
+fa_status_t fa_fwd_prefix(const void *q, const void *k_prefix, const void *v_prefix, const void *k, const void *v,
+                          void *o, float *lse, const int *seqlens_k, int B, int Hq, int Hkv, int Nq, int Np, int Nk,
+                          int D, int causal, float scale, void *stream, fa_dtype_t in_dtype, fa_dtype_t out_dtype,
+                          void *workspace, size_t workspace_bytes) {
+    return prefix(q, k_prefix, v_prefix, k, v, o, lse, seqlens_k, B, Hq, Hkv, Nq, Np, Nk, D, causal, scale, stream,
+                  in_dtype, out_dtype, Paging(), workspace, workspace_bytes);
+}
+
+fa_status_t fa_fwd_prefix_paged(const void *q, const void *k_pages, const void *v_pages, void *o, float *lse,
+                                const int *seqlens_k, const int *block_table, int B, int Hq, int Hkv, int Nq, int D,
+                                int page_size, int max_pages, int num_pages, int prefix_len, int causal, float scale,
+                                void *stream, fa_dtype_t in_dtype, fa_dtype_t out_dtype, void *workspace,
+                                size_t workspace_bytes) {
+    if (!seqlens_k || !block_table) return FA_ERR_NULL;
+    if (!pages_ok(B, page_size, max_pages, num_pages)) return FA_ERR_DIM;
+    if (prefix_len < page_size || prefix_len % page_size != 0 || prefix_len > page_size * max_pages) return FA_ERR_DIM;
+    Paging pg;
+    pg.block_table = block_table;
+    pg.page_size = page_size;
+    pg.max_pages = max_pages;
+    pg.num_pages = num_pages;
+    return prefix(q, k_pages, v_pages, k_pages, v_pages, o, lse, seqlens_k, B, Hq, Hkv, Nq, prefix_len,
+                  page_size * max_pages - prefix_len, D, causal, scale, stream, in_dtype, out_dtype, pg, workspace,
+                  workspace_bytes);
+}
+
+size_t fa_prefix_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Np, int Nk, int D, fa_dtype_t in_dtype) {
+    if (B < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || Nq < 1 || Np < 1 || Nk < 0 || (D != 64 && D != 128) ||
+        (long long)Np + Nk > FA_MAX_PREFIX_KEYS || (in_dtype != FA_F16 && in_dtype != FA_BF16) ||
+        (long long)B * Nq > 0x7fffffffLL || (long long)B * Nq * Hq > 0x7fffffffLL)
+        return 0;
+    return fa::prefix_workspace_bytes(B, Hq, Hkv, Nq, Np, Nk, D, true);
 }
 
 fa_status_t fa_kvcache_append(const void *k, const void *v, void *k_cache, void *v_cache, const void *q,

@@ -487,6 +487,20 @@ hipError_t launch_t(const Problem &p, int S, void *ws, hipStream_t stream) {
     return hipGetLastError();
 }
 
+template <typename TIN, int D>
+hipError_t launch_part(const Problem &p, int S, int slots, int slot0, int first, void *ws, hipStream_t stream) {
+    DecodeArgs a;
+    const long long nblocks = split_args<D>(p, S, slots, ws, a);
+    if (nblocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    a.first = first;
+    a.slot0 = slot0;
+    if (p.block_table)
+        hipLaunchKernelGGL((decode_split_kernel<TIN, D, true, true>), dim3((unsigned)nblocks), dim3(64 * NW), 0, stream, a);
+    else
+        hipLaunchKernelGGL((decode_split_kernel<TIN, D, false, true>), dim3((unsigned)nblocks), dim3(64 * NW), 0, stream, a);
+    return hipGetLastError();
+}
+
 template <typename TIN, typename TOUT>
 hipError_t launch_d(const Problem &p, int S, void *ws, hipStream_t s) {
     return p.D == 64 ? launch_t<TIN, TOUT, 64>(p, S, ws, s) : launch_t<TIN, TOUT, 128>(p, S, ws, s);
@@ -562,6 +576,14 @@ int decode_most_splits(int B, int Hq, int Hkv, int Nk, int D) {
 
 size_t decode_workspace_bytes(int B, int Hq, int D, int splits) {
     return (size_t)B * Hq * splits * (size_t)(D + 2) * sizeof(float);
+}
+
+hipError_t launch_decode_part(const Problem &p, int splits, int slots, int slot0, int first, void *ws, hipStream_t s) {
+    if (p.in == FA_F16)
+        return p.D == 64 ? launch_part<f16_t, 64>(p, splits, slots, slot0, first, ws, s)
+                         : launch_part<f16_t, 128>(p, splits, slots, slot0, first, ws, s);
+    return p.D == 64 ? launch_part<bf16_t, 64>(p, splits, slots, slot0, first, ws, s)
+                     : launch_part<bf16_t, 128>(p, splits, slots, slot0, first, ws, s);
 }
 
 hipError_t launch_decode(const Problem &p, int splits, void *ws, hipStream_t stream) {
