@@ -391,8 +391,9 @@ def fwd_prefix_paged(q, k_pages, v_pages, block_table, seqlens_k, prefix_len: in
                      scale: float | None = None, out=None, lse=None, out_dtype=None, return_lse: bool = True,
                      workspace=None):
     """``fwd_kvcache_paged`` for sequences whose first ``prefix_len`` keys (a
-    multiple of the page size) lie in the same pages, those of ``block_table[0]``:
-    these are read once for the whole batch (fa_fwd_prefix_paged)."""
+    multiple of the page size) lie in the same pages, which every row of
+    ``block_table`` names: these are read once for the whole batch
+    (fa_fwd_prefix_paged)."""
     lib = _lib.load()
     rt = _runtime()
     dims, out, lse, odt = _prepare_paged(rt, q, k_pages, v_pages, block_table, seqlens_k, out, lse, out_dtype, return_lse)

@@ -343,7 +343,9 @@ fa_status_t prefix(const void *q, const void *k_prefix, const void *v_prefix, co
     const size_t need = fa::prefix_workspace_bytes(B, Hq, Hkv, Nq, Np, Nk, D, false);
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     bool user = workspace || workspace_bytes;
-    if (user) {
+    if (need == 0) {   // one pass: no workspace
+        user = false;
+    } else if (user) {
         if (!workspace) return FA_ERR_NULL;
         if (fa::misaligned(workspace, 16)) return FA_ERR_ALIGN;
         if (workspace_bytes < need) return FA_ERR_WORKSPACE;

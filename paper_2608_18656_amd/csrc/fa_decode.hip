@@ -66,9 +66,7 @@ struct DecodeArgs {
     const int *block_table;   // paged K/V: page of each key block (see Problem)
     Divisor page_size;
     int max_pages, num_pages;
-    // RANGED: the keys from max(first, length - window) on, and the first `sinks`
-    int first, window, sinks;
-    int slots, slot0;   // partial results of a row that the workspace holds; this launch's first
+    int window, sinks;   // WIN: the last `window` keys and the first `sinks`
 };
 
 template <int D> struct DSmem {
@@ -86,7 +84,7 @@ __device__ __forceinline__ void wave_lds_fence() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-template <typename TIN, int D, bool PAGED, bool RANGED = false>
+template <typename TIN, int D, bool PAGED, bool WIN = false>
 __global__ __launch_bounds__(64 * NW, 1) void decode_split_kernel(DecodeArgs a) {
     using S = typename TIN::scalar;
     using V8 = typename TIN::vec8;
@@ -113,7 +111,7 @@ __global__ __launch_bounds__(64 * NW, 1) void decode_split_kernel(DecodeArgs a) 
     // once, one workgroup for every CU, the others shortest first.  Ranking
     // takes some 0.5 us: below 512 keys a split it is not done (13 x 32/8
     // heads, 1050 keys, D = 64, 4 splits 11.7 us against 12.3 with it)
-    if (!RANGED && a.ranked > 0) {
+    if (!WIN && a.ranked > 0) {
         const Lengths lens(a.seqlens, a.B, l);
         if (lens.uneven()) b = lens.nth_longest(b < a.ranked ? b : a.B - 1 - (b - a.ranked));
         len = lens.of(b);
@@ -126,14 +124,14 @@ __global__ __launch_bounds__(64 * NW, 1) void decode_split_kernel(DecodeArgs a) 
     const int Nk = __builtin_amdgcn_readfirstlane(min(max(len, 0), a.Nk));
     const unsigned whole = a.S.div(Nk), per = whole + (whole * a.S.d != (unsigned)Nk);   // ceil(Nk / S)
     const long long chunk = (per + (KPW - 1)) & ~(unsigned)(KPW - 1);
-    const int k0 = RANGED ? 0 : (int)min(s * chunk, (long long)Nk);
-    const int k1 = RANGED ? Nk : (int)min(k0 + chunk, (long long)Nk);
-    // RANGED: of the chunks that hold a visible key (those of the sinks, `near`,
+    const int k0 = WIN ? 0 : (int)min(s * chunk, (long long)Nk);
+    const int k1 = WIN ? Nk : (int)min(k0 + chunk, (long long)Nk);
+    // WIN: of the chunks that hold a visible key (those of the sinks, `near`,
     // and those from near + gap on) the split's share, from the chunk0-th one.
     // The keys between, from the last sink to first_key, count as not there.
     int near = 0, gap = 0, chunk0 = 0, share = 0, first_key = 0, sinks = 0;
-    if constexpr (RANGED) {
-        first_key = max(a.first, Nk - a.window);
+    if constexpr (WIN) {
+        first_key = max(Nk - a.window, 0);
         sinks = min(a.sinks, first_key);
         near = (sinks + KPW - 1) / KPW;
         gap = max(first_key / KPW - near, 0);
@@ -143,7 +141,7 @@ __global__ __launch_bounds__(64 * NW, 1) void decode_split_kernel(DecodeArgs a) 
         share = min(each, n - chunk0);
     }
     auto first_of = [&](int ch) {   // first key of the workgroup's ch-th chunk
-        if constexpr (!RANGED) return k0 + ch * KPW;
+        if constexpr (!WIN) return k0 + ch * KPW;
         const int c = chunk0 + ch;
         return (c + (c >= near ? gap : 0)) * KPW;
     };
@@ -189,7 +187,7 @@ __global__ __launch_bounds__(64 * NW, 1) void decode_split_kernel(DecodeArgs a) 
     int off[RLOADS];
 #pragma unroll
     for (int i = 0; i < RLOADS; ++i) off[i] = (l + 64 * i) / CPR * row_bytes + 16 * ((l + 64 * i) % CPR);
-    const int nchunks = RANGED ? share : (k1 - k0 + KPW - 1) / KPW;
+    const int nchunks = WIN ? share : (k1 - k0 + KPW - 1) / KPW;
     uint4_t kr[RLOADS], vr[RLOADS];   // the next chunk's rows, in flight
     auto gload = [&](int ch) __attribute__((always_inline)) {
         // first key of the chunk (past the last chunk: an empty view)
@@ -217,7 +215,7 @@ __global__ __launch_bounds__(64 * NW, 1) void decode_split_kernel(DecodeArgs a) 
 #pragma unroll
         for (int i = 0; i < RLOADS; ++i) {
             int at = off[i];
-            if constexpr (RANGED) {   // keys between read as zeros
+            if constexpr (WIN) {   // keys between read as zeros
                 const int key = kb + (l + 64 * i) / CPR;
                 at = key >= sinks && key < first_key ? (int)0x80000000 : at;
             }
@@ -250,8 +248,8 @@ __global__ __launch_bounds__(64 * NW, 1) void decode_split_kernel(DecodeArgs a) 
             s1 = mfma16(as_vec8<V8>(*reinterpret_cast<const uint4_t *>(kl + 16 * SM::KS + 32 * ks)),
                         qf[ks], s1);
         }
-        const bool masked = kb + KPW > k1 || (RANGED && kb < first_key && kb + KPW > sinks);
-        auto seen = [&](int key) { return key < k1 && (!RANGED || key >= first_key || key < sinks); };
+        const bool masked = kb + KPW > k1 || (WIN && kb < first_key && kb + KPW > sinks);
+        auto seen = [&](int key) { return key < k1 && (!WIN || key >= first_key || key < sinks); };
         if (masked) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
@@ -331,8 +329,8 @@ __global__ __launch_bounds__(64 * NW, 1) void decode_split_kernel(DecodeArgs a) 
             L += wgt[ww] * mf[(ww * QG + mq) * (D + 2) + D + 1];
         }
         const size_t bh = (size_t)b * a.Hq + g * G + mh;
-        const bool direct = RANGED ? a.slots == 1 : a.S.d == 1;   // one split: the result itself
-        const size_t slot = RANGED ? bh * a.slots + a.slot0 + s : bh * a.S.d + s;   // (bh itself with one split)
+        const bool direct = a.S.d == 1;   // one split: the result itself
+        const size_t slot = bh * a.S.d + s;   // (bh itself with one split)
         // as the merge does: a sequence with no valid key (per-sequence lengths),
         // or whose scores are not numbers, gives 0 and -inf
         const bool some = !direct || L > 0.f;
@@ -418,11 +416,11 @@ __global__ __launch_bounds__(D) void decode_combine_kernel(const float *__restri
 // Workgroups that the chip holds at once.
 constexpr long long resident(int D) { return D == 64 ? 2 * CUS : CUS; }
 
-// The first kernel's arguments for S splits; the workspace holds `slots` partial results of a row.
-template <int D>
-long long split_args(const Problem &p, int S, int slots, void *ws, DecodeArgs &a) {
+template <typename TIN, typename TOUT, int D>
+hipError_t launch_t(const Problem &p, int S, void *ws, hipStream_t stream) {
+    DecodeArgs a;
     a.q = p.q; a.k = p.k; a.v = p.v;
-    const size_t nslot = (size_t)p.B * p.Hq * slots;
+    const size_t nslot = (size_t)p.B * p.Hq * S;
     a.opart = reinterpret_cast<float *>(ws);
     a.mpart = a.opart + nslot * D;
     a.lpart = a.mpart + nslot;
@@ -442,62 +440,30 @@ long long split_args(const Problem &p, int S, int slots, void *ws, DecodeArgs &a
     a.page_size = Divisor(p.block_table ? p.page_size : 1);
     a.max_pages = p.max_pages;
     a.num_pages = p.num_pages;
+    a.window = p.window;
+    a.sinks = p.sinks;
+    const long long nblocks = (long long)p.B * p.Hkv * nqg * S;
+    if (nblocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
     a.B = p.B;
     a.ranked = 0;
-    a.first = a.sinks = a.slot0 = 0;
-    a.window = 0x7fffffff;
-    a.slots = slots;
-    return (long long)p.B * p.Hkv * nqg * S;
-}
-
-template <typename TIN, typename TOUT, int D>
-hipError_t launch_t(const Problem &p, int S, void *ws, hipStream_t stream) {
-    DecodeArgs a;
-    const long long nblocks = split_args<D>(p, S, S, ws, a);
-    if (nblocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-    if (p.window > 0) {
-        a.window = p.window;
-        a.sinks = p.sinks;
-        if (p.block_table)
-            hipLaunchKernelGGL((decode_split_kernel<TIN, D, true, true>), dim3((unsigned)nblocks), dim3(64 * NW), 0,
-                               stream, a);
-        else
-            hipLaunchKernelGGL((decode_split_kernel<TIN, D, false, true>), dim3((unsigned)nblocks), dim3(64 * NW), 0,
-                               stream, a);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess || S == 1) return e;
-        hipLaunchKernelGGL((decode_combine_kernel<TOUT, D>), dim3((unsigned)(p.B * p.Hq)), dim3(D), 0,
-                           stream, a.opart, a.mpart, a.lpart, p.o, p.lse, S);
-        return hipGetLastError();
-    }
-    if (p.seqlens && p.B > 1 && p.B <= kMaxRanked && nblocks > CUS && p.Nk >= RANKED_KEYS * (long long)S) {
+    if (p.window == 0 && p.seqlens && p.B > 1 && p.B <= kMaxRanked && nblocks > CUS &&
+        p.Nk >= RANKED_KEYS * (long long)S) {
         const long long per_seq = nblocks / p.B;
         a.ranked = nblocks <= resident(D) ? (int)((CUS + per_seq - 1) / per_seq) : p.B;
     }
-    if (p.block_table)
-        hipLaunchKernelGGL((decode_split_kernel<TIN, D, true>), dim3((unsigned)nblocks), dim3(64 * NW), 0,
-                           stream, a);
+    const dim3 grid((unsigned)nblocks), block(64 * NW);
+    if (p.window > 0 && p.block_table)
+        hipLaunchKernelGGL((decode_split_kernel<TIN, D, true, true>), grid, block, 0, stream, a);
+    else if (p.window > 0)
+        hipLaunchKernelGGL((decode_split_kernel<TIN, D, false, true>), grid, block, 0, stream, a);
+    else if (p.block_table)
+        hipLaunchKernelGGL((decode_split_kernel<TIN, D, true>), grid, block, 0, stream, a);
     else
-        hipLaunchKernelGGL((decode_split_kernel<TIN, D, false>), dim3((unsigned)nblocks), dim3(64 * NW), 0,
-                           stream, a);
+        hipLaunchKernelGGL((decode_split_kernel<TIN, D, false>), grid, block, 0, stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || S == 1) return e;
     hipLaunchKernelGGL((decode_combine_kernel<TOUT, D>), dim3((unsigned)(p.B * p.Hq)), dim3(D), 0,
                        stream, a.opart, a.mpart, a.lpart, p.o, p.lse, S);
-    return hipGetLastError();
-}
-
-template <typename TIN, int D>
-hipError_t launch_part(const Problem &p, int S, int slots, int slot0, int first, void *ws, hipStream_t stream) {
-    DecodeArgs a;
-    const long long nblocks = split_args<D>(p, S, slots, ws, a);
-    if (nblocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-    a.first = first;
-    a.slot0 = slot0;
-    if (p.block_table)
-        hipLaunchKernelGGL((decode_split_kernel<TIN, D, true, true>), dim3((unsigned)nblocks), dim3(64 * NW), 0, stream, a);
-    else
-        hipLaunchKernelGGL((decode_split_kernel<TIN, D, false, true>), dim3((unsigned)nblocks), dim3(64 * NW), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -576,14 +542,6 @@ int decode_most_splits(int B, int Hq, int Hkv, int Nk, int D) {
 
 size_t decode_workspace_bytes(int B, int Hq, int D, int splits) {
     return (size_t)B * Hq * splits * (size_t)(D + 2) * sizeof(float);
-}
-
-hipError_t launch_decode_part(const Problem &p, int splits, int slots, int slot0, int first, void *ws, hipStream_t s) {
-    if (p.in == FA_F16)
-        return p.D == 64 ? launch_part<f16_t, 64>(p, splits, slots, slot0, first, ws, s)
-                         : launch_part<f16_t, 128>(p, splits, slots, slot0, first, ws, s);
-    return p.D == 64 ? launch_part<bf16_t, 64>(p, splits, slots, slot0, first, ws, s)
-                     : launch_part<bf16_t, 128>(p, splits, slots, slot0, first, ws, s);
 }
 
 hipError_t launch_decode(const Problem &p, int splits, void *ws, hipStream_t stream) {

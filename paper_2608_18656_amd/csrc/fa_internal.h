@@ -36,7 +36,7 @@ struct PrefixProblem {
     Problem p;
     const void *k_prefix, *v_prefix;   // [Np][Hkv][D]; paged: the pools
     int Np;            // keys of the prefix
-    int suffix_rows;   // keys that a suffix can hold
+    int own;           // keys that a sequence can have of its own
 };
 
 // New keys and values into a cache, with the rotation by positions (fa_kvcache_append).
@@ -63,9 +63,6 @@ hipError_t launch_generic_window(const Problem &p, hipStream_t stream);
 hipError_t launch_decode(const Problem &p, int splits, void *workspace, hipStream_t stream);
 hipError_t launch_unfused(const Problem &p, void *workspace, hipStream_t stream);
 hipError_t launch_prefix(const PrefixProblem &p, void *workspace, hipStream_t stream);
-// Partial results of keys `first` and on, splits of them in the workspace's slots from slot0 on, of `slots` a row.
-hipError_t launch_decode_part(const Problem &p, int splits, int slots, int slot0, int first, void *workspace,
-                              hipStream_t stream);
 hipError_t launch_append(const AppendProblem &p, hipStream_t stream);
 hipError_t launch_q8_gemv(const void *w, const void *x, void *y, int M, int K, fa_dtype_t x_dtype,
                           fa_dtype_t y_dtype, hipStream_t stream);
@@ -77,7 +74,7 @@ int decode_default_splits(int B, int Hq, int Hkv, int Nk, int D);
 int decode_most_splits(int B, int Hq, int Hkv, int Nk, int D);   // of any cache of up to Nk keys
 size_t decode_workspace_bytes(int B, int Hq, int D, int splits);
 
-// Partial results of prefix and suffix; most: enough for every shorter one as well.
+// Partial results of prefix and suffix (0: one pass); most: enough for every shorter one as well.
 size_t prefix_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Np, int Nk, int D, bool most);
 
 // Unfused path: supported shapes and the workspace it needs (0 when a size is

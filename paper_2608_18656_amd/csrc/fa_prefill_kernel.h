@@ -75,12 +75,13 @@ constexpr float kMaxLaneSum = 4096.0f;   // largest 16-weight lane sum kept with
 //   WINDOW  the `window` keys up to the row's own and the first `sinks` (causal):
 //           tiles between the two parts are not visited, nor are a tile's keys
 //           that a wave's rows do not see multiplied
-//   PREFIX  keys that all sequences share, a split of them: the B Nq G rows of a
-//           key/value head are numbered together (row of token t and head e of
-//           the group: t G + e) and take their own split's part of the keys
-//   SUFFIX  each sequence's keys past the shared ones
-// PREFIX and SUFFIX leave partial results (accumulator, base, sum) for a merge.
-enum { ALL = 0, WINDOW = 1, PREFIX = 2, SUFFIX = 3 };
+//   PARTS   sequences that share a prefix, their keys in parts: workgroups of the
+//           prefix, whose rows are those of all sequences, and workgroups of one
+//           sequence's own keys, both a split of the keys.  The B Nq G rows of a
+//           key/value head are numbered together (token t, head e of the group:
+//           row t G + e).  Each leaves a partial result (accumulator, base, sum).
+//   JOIN    the shared keys, then the sequence's own
+enum { ALL = 0, WINDOW = 1, PARTS = 2, JOIN = 3 };
 
 struct PrefillArgs {
     const void *q, *k, *v;
@@ -106,15 +107,19 @@ struct PrefillArgs {
     // all but ALL
     Divisor page_div;     // page_size
     int window, sinks;    // WINDOW: at most Nk each
-    Divisor tokens, group;   // PREFIX: Nq, G
-    int rows;             // PREFIX: B Nq G
-    int splits, per_split;   // PREFIX: splits of the keys, tiles in each
-    int causal;           // PREFIX
-    int total;            // PREFIX: keys that a sequence can hold (prefix and suffix)
-    int length0;          // added to the lengths: PREFIX: keys that they do not count; SUFFIX: minus the prefix's that they do
-    int first_page;       // SUFFIX: table entry of the suffix's first page
-    float *opart, *mpart, *lpart;   // partial results: [token][head][slots], the accumulators D columns each
-    int slots, slot0;     // partial results of a row; the first that this launch writes
+    // PARTS, JOIN: k, v and Nk are the sequences' own keys (paged: of all)
+    const void *k_prefix, *v_prefix;
+    int prefix;           // keys of the prefix
+    int own;              // keys that a sequence can have of its own
+    int counted;          // keys of the prefix that the lengths count: prefix, or 0
+    // PARTS
+    int first_page;       // table entry of a sequence's own first page
+    int causal, rows;     // rows: B Nq G
+    int prefix_blocks;    // workgroups of the prefix, ahead of the others
+    Divisor splits, own_splits;   // of the prefix's keys and of a sequence's own
+    Divisor batch, tokens, group;   // B, Nq, G
+    float *opart, *mpart, *lpart;   // [token][head][slots] partial results: the prefix's, then the own ones
+    int slots;
 };
 
 // Tile shape per head size.  Every wave handles 32 query rows and 32 keys of
@@ -152,6 +157,11 @@ template <int D, int NS = NSLOT> struct Cfg {
     static constexpr int NP = SPLIT ? 1 : PIECES / NWG;
     static_assert(PIECES == 8 && (SPLIT ? NWG == 2 * PIECES : PIECES % NWG == 0), "staging split");
 };
+
+// Valid keys that sequence b has of its own (PARTS, JOIN).
+__device__ __forceinline__ int own_keys(const PrefillArgs &a, int b) {
+    return a.seqlens ? min(max(min(max(a.seqlens[b], 0), a.prefix + a.own) - a.counted, 0), a.own) : a.own;
+}
 
 template <typename TIN, typename TOUT, int D, int NS, bool CAUSAL, bool PAGED, int MODE = ALL>
 __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_eu((Cfg<D, NS>::WPE), (Cfg<D, NS>::WPE)))) void prefill_kernel(PrefillArgs a) {
@@ -211,25 +221,43 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
         len = lens.of(b);
     }
     const int bg = a.nhg.div(rest), hg = rest - bg * a.nhg.d;
-    const int b0 = a.nkv.div(bg), g = bg - b0 * a.nkv.d;
+    int b0 = a.nkv.div(bg), g = bg - b0 * a.nkv.d;
+    // PARTS: the prefix's workgroups, or a sequence's: split, rows and their bounds
+    bool own = false;
+    int split = 0, nsplit = 1, part_row0 = 0, part_rows = 0;
+    if constexpr (MODE == PARTS) {
+        own = bid >= a.prefix_blocks;
+        const int r = own ? bid - a.prefix_blocks : bid;
+        const int u = own ? a.own_splits.div(r) : a.splits.div(r);
+        nsplit = own ? a.own_splits.d : a.splits.d;
+        split = r - u * nsplit;
+        const int t = a.nkv.div(u);
+        g = u - t * a.nkv.d;
+        mb = own ? (int)a.batch.div(t) : t;
+        b0 = own ? t - mb * (int)a.batch.d : 0;
+        part_row0 = b0 * a.Nq * a.G;
+        part_rows = own ? part_row0 + a.Nq * a.G : a.rows;
+    }
     if (MODE != ALL || a.ranked == 0) {
         b = b0;
-        if (MODE != PREFIX && a.seqlens) len = a.seqlens[b];
-        if (MODE == SUFFIX) len = max(len, 0) + a.length0;
+        if (MODE != PARTS && a.seqlens) len = a.seqlens[b];
     }
     const int G = a.G;
     const int hs = slot & (a.HW - 1), rs = slot >> a.lgHW;
-    const int row0_wg = mb * (WR * RB);
+    const int row0_wg = mb * (WR * RB) + part_row0;
     const int row0 = row0_wg + rs * WR;
     const int qi = row0 + lq;
-    const int Nq = MODE == PREFIX ? a.rows : a.Nq;
-    // PREFIX: hg is the split, the rows are tokens and heads
-    const int tok = MODE == PREFIX ? (int)a.group.div(min(qi, Nq - 1)) : 0;
-    const int h = MODE == PREFIX ? g * G + (min(qi, Nq - 1) - tok * G) : g * G + hg * a.HW + hs;
+    const int Nq = MODE == PARTS ? part_rows : a.Nq;
+    const int tok = MODE == PARTS ? (int)a.group.div(min(qi, Nq - 1)) : 0;   // the row's token (PARTS)
+    const int h = MODE == PARTS ? g * G + (min(qi, Nq - 1) - tok * G) : g * G + hg * a.HW + hs;
     // Valid keys of this batch element: with per-sequence lengths the K/V
     // tensors hold a.Nk rows per batch element of which the first seqlens[b]
     // are valid, and the queries are the sequence's last Nq positions.
-    const int Nk = __builtin_amdgcn_readfirstlane(min(max(len, 0), a.Nk));
+    // PARTS: of the part: the prefix's or the sequence's own.  JOIN: of both.
+    int valid = min(max(len, 0), a.Nk);
+    if constexpr (MODE == PARTS) valid = own ? own_keys(a, b0) : a.prefix;
+    if constexpr (MODE == JOIN) valid = a.prefix + own_keys(a, b);
+    const int Nk = __builtin_amdgcn_readfirstlane(valid);
     const int off = Nk - Nq;
 
     // Key extents: workgroup, this slot, and keys every row of the slot sees.
@@ -242,34 +270,41 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
     // WINDOW: the sinks' and, from the first row's window on, the others; the
     // keys between, from the last sink to first_key, count as not there, so that
     // what they hold has no part in the result.
+    // JOIN: the prefix's tiles are the first `near`, the own ones follow.
     int near = 0, gap = 0, first_key = 0;
-    int rlim = 0;   // PREFIX: keys of the prefix that the lane's row sees
+    int rlim = 0;   // PARTS: keys of the part that the lane's row sees
     if constexpr (MODE == WINDOW) {
         first_key = max(row0_wg + off + 1 - a.window, 0);
         near = max((min(a.sinks, kend_wg) + BC - 1) / BC, 0);
         gap = max(first_key / BC - near, 0);
         ntiles -= gap;
     }
-    if constexpr (MODE == PREFIX) {
-        near = 0;
-        gap = min(hg * a.per_split, ntiles);
-        ntiles = min(ntiles - gap, a.per_split);
+    if constexpr (MODE == PARTS) {
+        const int each = (ntiles + nsplit - 1) / nsplit;
+        gap = min(split * each, ntiles);
+        ntiles = min(ntiles - gap, each);
+        const int sb = a.tokens.div(tok), i = tok - sb * a.Nq;
         rlim = Nk;
-        if (a.seqlens || a.causal) {
-            const int sb = a.tokens.div(tok), i = tok - sb * a.Nq;
-            int n = a.total;   // keys of the sequence
-            if (a.seqlens) n = min(min(max(a.seqlens[sb], 0), a.total) + a.length0, a.total);
+        if (own) {
+            if (a.causal) rlim = min(Nk - a.Nq + i + 1, Nk);
+        } else if (a.causal || a.counted) {   // rows that lie in the prefix, sequences shorter than it
+            int n = a.prefix + a.own;
+            if (a.seqlens) n = min(min(max(a.seqlens[sb], 0), n) + a.prefix - a.counted, n);
             rlim = a.causal ? min(n - a.Nq + i + 1, Nk) : min(n, Nk);
         }
-        // some row does not see all of the prefix: every tile is masked
+        // some row does not see all of the part: every tile is masked
         if (__builtin_amdgcn_ballot_w64(rlim < Nk)) kfree_w = 0;
+    }
+    if constexpr (MODE == JOIN) {
+        near = (a.prefix + BC - 1) / BC;
+        if (kend_wg > a.prefix) ntiles = near + (kend_wg - a.prefix + BC - 1) / BC;
     }
 
     // Q rows of this lane (B operand of S^T = K Q^T).
     V8 qf[KSTEPS];
     {
         const int qrow = min(qi, Nq - 1);
-        const size_t qtok = MODE == PREFIX ? (size_t)tok : (size_t)b * Nq + qrow;
+        const size_t qtok = MODE == PARTS ? (size_t)tok : (size_t)b * Nq + qrow;
         const S *qp = reinterpret_cast<const S *>(a.q) + (qtok * a.Hq + h) * D + 8 * lh;
 #pragma unroll
         for (int ks = 0; ks < KSTEPS; ++ks) {
@@ -310,12 +345,16 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
     // buffer view of a tile ends after its last valid key (keys past it read
     // as zero): a full tile's extent for the first Nk / BC tiles, then that of
     // the remaining keys, if any (one tile's extent fits 31 bits: tile_fits).
-    const size_t head0 = ((size_t)(MODE == PREFIX ? 0 : b) * a.Nk * a.Hkv + g) * D;
-    const S *ktile = reinterpret_cast<const S *>(a.k) + (PAGED ? 0 : head0);
-    const S *vtile = reinterpret_cast<const S *>(a.v) + (PAGED ? 0 : head0);
+    const bool prefix_first = MODE == JOIN || (MODE == PARTS && !own);   // the first tile is one of the prefix
+    const size_t head0 = ((size_t)(MODE == PARTS ? b0 : b) * a.Nk * a.Hkv + g) * D;
+    const S *kbase = reinterpret_cast<const S *>(prefix_first ? a.k_prefix : a.k);
+    const S *vbase = reinterpret_cast<const S *>(prefix_first ? a.v_prefix : a.v);
+    const S *ktile = kbase + (PAGED ? 0 : prefix_first ? (size_t)g * D : head0);
+    const S *vtile = vbase + (PAGED ? 0 : prefix_first ? (size_t)g * D : head0);
     const int tile_bytes = (BC - 1) * row_bytes + D * (int)sizeof(S);
-    const int full_tiles = Nk / BC;
-    const int last_bytes = Nk % BC ? (Nk % BC - 1) * row_bytes + D * (int)sizeof(S) : 0;
+    auto bytes_of = [&](int rows) { return rows > 0 ? (rows - 1) * row_bytes + D * (int)sizeof(S) : 0; };
+    int full_tiles = MODE == JOIN ? a.prefix / BC : Nk / BC;
+    int last_bytes = bytes_of(MODE == JOIN ? a.prefix % BC : Nk % BC);
     int tload = 0;
     // paged K/V: the pool of pages, at head g.  Tiles are loaded in order
     // and a page holds a whole number of tiles, so the page index and the
@@ -327,9 +366,9 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
     // of two tiles, where it would wait for the tiles as well (with the entry
     // of the following page loaded alone, 5 x 32/4 heads, 61 rows, 7680 keys,
     // D = 64, pages of 64 took 115 us against 78 for contiguous keys).
-    const int page0 = MODE == SUFFIX ? a.first_page : 0;
+    const int page0 = MODE == PARTS && own ? a.first_page : 0;
     const __amdgpu_buffer_rsrc_t trs = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<int *>(PAGED ? a.block_table + (MODE == PREFIX ? 0 : (size_t)b * a.max_pages + page0) : nullptr), (short)0,
+        const_cast<int *>(PAGED ? a.block_table + (size_t)(MODE == PARTS ? b0 : b) * a.max_pages + page0 : nullptr), (short)0,
         PAGED ? (a.max_pages - page0) * 4 : 0, 0x00020000);
     const size_t page_elems = (size_t)a.page_size * row_elems;
     int pidx = 0, poff = 0;   // page index and key offset of the next tile
@@ -351,15 +390,23 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
             tnx = __builtin_amdgcn_raw_buffer_load_b32(trs, at + 256, 0, 0);
             const int page = min(max(__builtin_amdgcn_readlane(tcur, pidx % 64), 0), a.num_pages - 1);
             const size_t e = (size_t)g * D + (size_t)page * page_elems + (size_t)poff * row_elems;
-            ktile = reinterpret_cast<const S *>(a.k) + e;
-            vtile = reinterpret_cast<const S *>(a.v) + e;
+            ktile = kbase + e;
+            vtile = vbase + e;
         }
     };
     const unsigned lds0 = lds_address(smem);
     // the next tile (they are loaded in order) into stage `stage`; bf16 V into vr
     auto gload_to = [&](vregs_t &vr, int stage) __attribute__((always_inline)) {
-        if constexpr (MODE == WINDOW || MODE == PREFIX) {
+        if constexpr (MODE == WINDOW || MODE == PARTS) {
             if (gap > 0 && tload == near) go_to(near + gap);
+        }
+        if constexpr (MODE == JOIN) {
+            if (tload == near) {   // on to the sequence's own keys
+                ktile = reinterpret_cast<const S *>(a.k) + head0;
+                vtile = reinterpret_cast<const S *>(a.v) + head0;
+                full_tiles = near + (Nk - a.prefix) / BC;
+                last_bytes = bytes_of((Nk - a.prefix) % BC);
+            }
         }
         if constexpr (PAGED) {
             // the tile's rows sit in one page (pages hold a multiple of 64
@@ -367,14 +414,14 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
             // the address comes from the table (page numbers clamped into the
             // pool), within it the address advances by one tile per load
             if (poff == 0) {
-                if (pidx > 0 && pidx % 64 == 0 && MODE != WINDOW && MODE != PREFIX) {
+                if (pidx > 0 && pidx % 64 == 0 && MODE != WINDOW && MODE != PARTS) {
                     tcur = tnx;
                     tnx = __builtin_amdgcn_raw_buffer_load_b32(trs, 4 * (pidx + 64 + l), 0, 0);
                 }
                 const int page = min(max(__builtin_amdgcn_readlane(tcur, pidx % 64), 0), a.num_pages - 1);
                 const size_t t = (size_t)g * D + (size_t)page * page_elems;
-                ktile = reinterpret_cast<const S *>(a.k) + t;
-                vtile = reinterpret_cast<const S *>(a.v) + t;
+                ktile = kbase + t;
+                vtile = vbase + t;
             }
         }
         const int nrec = tload < full_tiles ? tile_bytes : last_bytes;
@@ -416,7 +463,7 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
             const bool cross = poff == a.page_size;   // wave-uniform
             poff = cross ? 0 : poff;
             pidx += cross ? 1 : 0;
-            if constexpr (MODE == WINDOW || MODE == PREFIX) {
+            if constexpr (MODE == WINDOW || MODE == PARTS) {
                 if (cross && pidx % 64 == 0) {
                     tcur = tnx;
                     tnx = __builtin_amdgcn_raw_buffer_load_b32(trs, 4 * (pidx + 64 + l), 0, 0);
@@ -549,15 +596,22 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
 
     // hide keys of tile t that some row of the wave must not see
     auto mask = [&](float16_t &s, int t) {
-        const int kw = t * BC + 32 * kh;        // first key of this wave's half
+        int kw = t * BC + 32 * kh;        // first key of this wave's half
+        int end = Nk;                     // keys from here on do not exist
+        if constexpr (MODE == JOIN) {
+            if (t < near)
+                end = a.prefix;
+            else
+                kw += a.prefix - near * BC;
+        }
         // WINDOW: the last key that the slot's last row does not see any more
         const int passed = MODE == WINDOW ? row0 + WR - 1 + off - a.window : -1;
-        if (kw + 32 > kfree_w || (MODE == WINDOW && kw <= passed && kw + 32 > a.sinks)) {
+        if (kw + 32 > (MODE == JOIN ? min(kfree_w, end) : kfree_w) || (MODE == WINDOW && kw <= passed && kw + 32 > a.sinks)) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int key = kw + 8 * (r >> 2) + 4 * lh + (r & 3);
-                const bool vis = MODE == PREFIX ? key < rlim
-                                                : key < Nk && (!CAUSAL || key <= qi + off) &&
+                const bool vis = MODE == PARTS ? key < rlim
+                                                : key < end && (!CAUSAL || key <= qi + off) &&
                                                       (MODE != WINDOW || key > qi + off - a.window || key < a.sinks);
                 s[r] = vis ? s[r] : -INFINITY;
             }
@@ -566,16 +620,21 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
 
     // p = 2^(s c + nbase) for the 16 scores of the lane, packed to f16 in the
     // key order of the two PV k-steps
+    float wsum = 0.f;   // all but ALL: the 16 weights' sum before they are rounded
     auto exp_pack = [&](const float16_t &s, float nbase, half8_t &p0, half8_t &p1) {
         float p[16];
 #pragma unroll
         for (int r = 0; r < 16; ++r) p[r] = exp2_fast(__builtin_fmaf(s[r], a.c, nbase));
+        if constexpr (MODE != ALL)
+            wsum = (((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]))) +
+                   (((p[8] + p[9]) + (p[10] + p[11])) + ((p[12] + p[13]) + (p[14] + p[15])));
         p0 = pack_f16x8(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7]);
         p1 = pack_f16x8(p[8], p[9], p[10], p[11], p[12], p[13], p[14], p[15]);
     };
 
     // row sum += the 16 f16 weights of the lane, in fp32 (dot products with (1, 1))
     auto add_sum = [&](float l, const half8_t &p0, const half8_t &p1) {
+        if constexpr (MODE != ALL) return l + wsum;
         const half2_t one = {(_Float16)1.0f, (_Float16)1.0f};
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -643,13 +702,13 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
         // the next tile's loads are issued after the K operand reads (their
         // scalar set-up then overlaps the LDS latency, and at D = 128 their
         // registers are not live across the QK^T product)
-        const int t = i + (MODE != ALL && i >= near ? gap : 0);   // the tile
+        const int t = i + ((MODE == WINDOW || MODE == PARTS) && i >= near ? gap : 0);   // the tile
         bool some = true;   // some row of the wave sees some key of it (wave-uniform)
         if constexpr (MODE == WINDOW) {
             const int kw = t * BC + 32 * kh;
             some = live && kw <= row0 + WR - 1 + off && (kw + 31 > row0 + off - a.window || kw < a.sinks);
         }
-        if constexpr (MODE == PREFIX) some = live;
+        if constexpr (MODE == PARTS) some = live;
         float16_t s;
         if (some) s = D == 128 ? scores_jit(stage_at(r)) : scores(stage_at(r));
         if (AHEAD == 2 && i + 1 < ntiles) {
@@ -716,10 +775,9 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
         m_run = M;
     }
     const float l_tot = pair_sum(l_run);
-    if constexpr (MODE == PREFIX || MODE == SUFFIX) {
+    if constexpr (MODE == PARTS) {
         if (qi >= Nq) return;
-        const size_t token = MODE == PREFIX ? (size_t)tok : (size_t)b * Nq + qi;
-        const size_t at = (token * a.Hq + h) * a.slots + a.slot0 + (MODE == PREFIX ? hg : 0);
+        const size_t at = ((size_t)tok * a.Hq + h) * a.slots + split + (own ? (int)a.splits.d : 0);
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll

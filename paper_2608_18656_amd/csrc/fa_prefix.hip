@@ -1,14 +1,19 @@
 // fa_prefix.hip -- attention of a batch whose sequences share a long prefix.
 //
-// softmax over prefix and suffix together is the sum of two parts, each an
+// softmax over prefix and suffix together is the sum of parts, each an
 // accumulator, a base and a sum (the state that streaming softmax carries from
 // key block to key block), so the parts can be taken apart:
 //   prefix  all B Nq G query rows of a key/value head against the prefix's keys,
 //           which are read once for every 128 rows instead of once a sequence
-//           (prefill kernel, PREFIX: 128 rows and a split of the keys a workgroup)
-//   suffix  each sequence's rows against its own keys (one row: the split-KV
-//           decode kernel; more: the prefill kernel, SUFFIX)
+//   own     each sequence's rows against its own keys
 //   merge   the parts by their bases, the final normalisation, the log-sum-exp
+// Prefix and own parts are workgroups of one launch (prefill kernel, PARTS), cut
+// into splits of the keys: the prefix's multiply while the others read.
+// Where a sequence's rows fill the 32 rows of a wave, the parts would share
+// nothing that the caches do not: then every row takes the prefix's keys and its
+// own in one pass (JOIN; paged caches: the paged prefill).
+#include <algorithm>
+
 #include "fa_checks.h"
 #include "fa_internal.h"
 #include "fa_prefill_kernel.h"
@@ -71,31 +76,36 @@ __global__ __launch_bounds__(256) void merge_kernel(const float *__restrict__ op
     }
 }
 
-// Splits of the prefix, and partial results of a row's suffix.
+// Splits of the prefix's keys and of a sequence's own.
 struct Plan {
-    int prefix, suffix;
+    int prefix, own;
 };
 
-int prefix_splits(long long rows, int Hkv, int Np, int D) {
-    const int BC = D == 64 ? Cfg<64>::BC : Cfg<128>::BC, wpc = D == 64 ? Cfg<64>::WPC : Cfg<128>::WPC;
-    const long long units = (rows + ROWS - 1) / ROWS * Hkv, tiles = ((long long)Np + BC - 1) / BC;
-    long long S = (long long)CUS * wpc / units;
-    if (S > tiles / MIN_TILES) S = tiles / MIN_TILES;
-    if (S > FA_MAX_SPLITS) S = FA_MAX_SPLITS;
-    return S < 1 ? 1 : (int)S;
-}
-
+// most: at least as many of both as any shorter prefix and suffix get.
 Plan plan(int B, int Hq, int Hkv, int Nq, int Np, int Nk, int D, bool most) {
-    Plan n;
-    n.prefix = prefix_splits((long long)B * Nq * (Hq / Hkv), Hkv, Np, D);
-    n.suffix = Nk < 1 ? 0 : Nq > 1 ? 1 : most ? decode_most_splits(B, Hq, Hkv, Nk, D) : decode_default_splits(B, Hq, Hkv, Nk, D);
-    return n;
+    const int BC = D == 64 ? Cfg<64>::BC : Cfg<128>::BC, wpc = D == 64 ? Cfg<64>::WPC : Cfg<128>::WPC;
+    const long long G = Hq / Hkv, rows = B * G * Nq;
+    const long long pu = (rows + ROWS - 1) / ROWS * Hkv, pt = (Np + BC - 1) / BC;
+    const long long su = (G * Nq + ROWS - 1) / ROWS * Hkv * B, st = (Nk + BC - 1) / BC;
+    const long long room = CUS * wpc;   // workgroups that the chip holds at once
+    long long each = (pu * pt + su * st + room - 1) / room;
+    if (each < MIN_TILES) each = MIN_TILES;
+    auto cut = [&](long long tiles, long long units) {
+        long long n = (tiles + each - 1) / each;
+        // (each >= units tiles / room, so n <= room / units + 1)
+        if (most) n = std::min((tiles + MIN_TILES - 1) / MIN_TILES, room / units + 1);
+        return n < 1 ? 1 : n > FA_MAX_SPLITS ? FA_MAX_SPLITS : (int)n;
+    };
+    return Plan{cut(pt, pu), Nk > 0 ? cut(st, su) : 0};
 }
 
-void common_args(const Problem &p, PrefillArgs &a) {
-    a.q = p.q;
-    a.o = p.o; a.lse = p.lse;
-    a.B = p.B; a.Hq = p.Hq; a.Hkv = p.Hkv; a.Nq = p.Nq;
+// Rows of a sequence from which its own pass over all keys is taken.
+bool one_pass(int Nq) { return Nq >= WR; }
+
+void common_args(const PrefixProblem &pp, PrefillArgs &a) {
+    const Problem &p = pp.p;
+    a.q = p.q; a.k = p.k; a.v = p.v; a.o = p.o; a.lse = p.lse;
+    a.B = p.B; a.Hq = p.Hq; a.Hkv = p.Hkv; a.Nq = p.Nq; a.Nk = p.Nk;
     a.seqlens = p.seqlens;
     a.block_table = p.block_table;
     a.page_size = p.page_size;
@@ -107,77 +117,72 @@ void common_args(const Problem &p, PrefillArgs &a) {
     a.G = p.Hq / p.Hkv;
     a.nkv = Divisor(p.Hkv);
     a.ranked = 0;
+    a.k_prefix = pp.k_prefix;
+    a.v_prefix = pp.v_prefix;
+    a.prefix = pp.Np;
+    a.own = pp.own;
+    a.counted = p.block_table ? pp.Np : 0;
 }
 
 template <typename TIN, int D>
 hipError_t launch_parts(const PrefixProblem &pp, const Plan &n, float *ws, hipStream_t stream) {
     using SM = Cfg<D>;
     const Problem &p = pp.p;
-    const int G = p.Hq / p.Hkv, slots = n.prefix + n.suffix;
+    const int G = p.Hq / p.Hkv;
     const long long rows = (long long)p.B * p.Nq * G;   // of a key/value head
-    const size_t parts = (size_t)rows * p.Hkv * slots;
-    const int total = pp.Np + pp.suffix_rows;
-
     PrefillArgs a;
-    common_args(p, a);
+    common_args(pp, a);
+    a.slots = n.prefix + n.own;
+    const size_t parts = (size_t)rows * p.Hkv * a.slots;
     a.opart = ws;
     a.mpart = ws + parts * D;
     a.lpart = a.mpart + parts;
-    a.slots = slots;
-
-    a.k = pp.k_prefix; a.v = pp.v_prefix;
-    a.Nk = pp.Np;
     a.HW = 1;
     a.lgHW = 0;
-    a.nmb = (int)((rows + ROWS - 1) / ROWS);
-    a.first = a.nmb;
-    a.nhg = Divisor(n.prefix);
-    a.per_mb = Divisor((unsigned)p.Hkv * n.prefix);
+    a.nmb = a.first = 0;
+    a.nhg = a.per_mb = Divisor(1);
+    a.causal = p.causal;
+    a.rows = (int)rows;
+    a.splits = Divisor(n.prefix);
+    a.own_splits = Divisor(n.own > 0 ? n.own : 1);
+    a.batch = Divisor(p.B);
     a.tokens = Divisor(p.Nq);
     a.group = Divisor(G);
-    a.rows = (int)rows;
-    a.splits = n.prefix;
-    const int tiles = (pp.Np + SM::BC - 1) / SM::BC;
-    a.per_split = (tiles + n.prefix - 1) / n.prefix;
-    a.causal = p.causal;
-    a.total = total;
-    a.length0 = p.block_table ? 0 : pp.Np;
-    a.slot0 = 0;
-    const long long nblocks = (long long)a.nmb * p.Hkv * n.prefix;
+    a.first_page = p.block_table ? pp.Np / p.page_size : 0;
+    const long long shared = (rows + ROWS - 1) / ROWS * p.Hkv * n.prefix;
+    const long long nblocks = shared + ((long long)p.Nq * G + ROWS - 1) / ROWS * p.B * p.Hkv * n.own;
     if (nblocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    a.prefix_blocks = (int)shared;
     if (p.block_table)
-        hipLaunchKernelGGL((prefill_kernel<TIN, float, D, NSLOT, false, true, PREFIX>), dim3((unsigned)nblocks),
+        hipLaunchKernelGGL((prefill_kernel<TIN, float, D, NSLOT, false, true, PARTS>), dim3((unsigned)nblocks),
                            dim3(SM::NT), 0, stream, a);
     else
-        hipLaunchKernelGGL((prefill_kernel<TIN, float, D, NSLOT, false, false, PREFIX>), dim3((unsigned)nblocks),
+        hipLaunchKernelGGL((prefill_kernel<TIN, float, D, NSLOT, false, false, PARTS>), dim3((unsigned)nblocks),
                            dim3(SM::NT), 0, stream, a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || n.suffix == 0) return e;
-    if (p.Nq == 1) return launch_decode_part(p, n.suffix, slots, n.prefix, p.block_table ? pp.Np : 0, ws, stream);
+    return hipGetLastError();
+}
 
-    a.k = p.k; a.v = p.v;
-    a.Nk = pp.suffix_rows;
+template <typename TIN, typename TOUT, int D>
+hipError_t launch_join(const PrefixProblem &pp, hipStream_t stream) {
+    using SM = Cfg<D>;
+    const Problem &p = pp.p;
+    PrefillArgs a;
+    common_args(pp, a);
+    const int G = a.G;
     a.HW = G % 4 == 0 ? 4 : G % 2 == 0 ? 2 : 1;
     a.lgHW = a.HW == 4 ? 2 : a.HW == 2 ? 1 : 0;
     const int RB = NSLOT / a.HW;
-    a.nmb = (p.Nq + WR * RB - 1) / (WR * RB);
-    a.first = a.nmb;
-    const long long sblocks = (long long)a.nmb * p.B * p.Hkv * (G / a.HW);
-    if (sblocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    a.nmb = a.first = (p.Nq + WR * RB - 1) / (WR * RB);
+    const long long nblocks = (long long)a.nmb * p.B * p.Hkv * (G / a.HW);
+    if (nblocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
     a.nhg = Divisor(G / a.HW);
     a.per_mb = Divisor((unsigned)p.B * p.Hkv * (G / a.HW));
-    a.length0 = p.block_table ? -pp.Np : 0;
-    a.first_page = p.block_table ? pp.Np / p.page_size : 0;
-    a.slot0 = n.prefix;
-    const dim3 grid((unsigned)sblocks), block(SM::NT);
-    if (p.block_table && p.causal)
-        hipLaunchKernelGGL((prefill_kernel<TIN, float, D, NSLOT, true, true, SUFFIX>), grid, block, 0, stream, a);
-    else if (p.block_table)
-        hipLaunchKernelGGL((prefill_kernel<TIN, float, D, NSLOT, false, true, SUFFIX>), grid, block, 0, stream, a);
-    else if (p.causal)
-        hipLaunchKernelGGL((prefill_kernel<TIN, float, D, NSLOT, true, false, SUFFIX>), grid, block, 0, stream, a);
+    if (p.causal)
+        hipLaunchKernelGGL((prefill_kernel<TIN, TOUT, D, NSLOT, true, false, JOIN>), dim3((unsigned)nblocks),
+                           dim3(SM::NT), 0, stream, a);
     else
-        hipLaunchKernelGGL((prefill_kernel<TIN, float, D, NSLOT, false, false, SUFFIX>), grid, block, 0, stream, a);
+        hipLaunchKernelGGL((prefill_kernel<TIN, TOUT, D, NSLOT, false, false, JOIN>), dim3((unsigned)nblocks),
+                           dim3(SM::NT), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -196,26 +201,31 @@ hipError_t launch_merge(const Problem &p, int slots, const float *ws, hipStream_
     return hipGetLastError();
 }
 
+template <typename TIN, typename TOUT>
+hipError_t launch_d(const PrefixProblem &pp, float *ws, hipStream_t stream) {
+    const Problem &p = pp.p;
+    if (one_pass(p.Nq))
+        return p.D == 64 ? launch_join<TIN, TOUT, 64>(pp, stream) : launch_join<TIN, TOUT, 128>(pp, stream);
+    const Plan n = plan(p.B, p.Hq, p.Hkv, p.Nq, pp.Np, pp.own, p.D, false);
+    const hipError_t e = p.D == 64 ? launch_parts<TIN, 64>(pp, n, ws, stream) : launch_parts<TIN, 128>(pp, n, ws, stream);
+    return e != hipSuccess ? e : launch_merge<TOUT>(p, n.prefix + n.own, ws, stream);
+}
+
 }  // namespace
 
 size_t prefix_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Np, int Nk, int D, bool most) {
+    if (one_pass(Nq)) return 0;
     const Plan n = plan(B, Hq, Hkv, Nq, Np, Nk, D, most);
-    return (size_t)B * Nq * Hq * (n.prefix + n.suffix) * (size_t)(D + 2) * sizeof(float);
+    return (size_t)B * Nq * Hq * (n.prefix + n.own) * (size_t)(D + 2) * sizeof(float);
 }
 
 hipError_t launch_prefix(const PrefixProblem &pp, void *workspace, hipStream_t stream) {
     const Problem &p = pp.p;
-    const Plan n = plan(p.B, p.Hq, p.Hkv, p.Nq, pp.Np, pp.suffix_rows, p.D, false);
+    if (p.block_table && one_pass(p.Nq)) return launch_prefill(p, stream);
     float *ws = reinterpret_cast<float *>(workspace);
-    hipError_t e;
     if (p.in == FA_F16)
-        e = p.D == 64 ? launch_parts<f16_t, 64>(pp, n, ws, stream) : launch_parts<f16_t, 128>(pp, n, ws, stream);
-    else
-        e = p.D == 64 ? launch_parts<bf16_t, 64>(pp, n, ws, stream) : launch_parts<bf16_t, 128>(pp, n, ws, stream);
-    if (e != hipSuccess) return e;
-    const int slots = n.prefix + n.suffix;
-    if (p.out == FA_F32) return launch_merge<float>(p, slots, ws, stream);
-    return p.in == FA_F16 ? launch_merge<_Float16>(p, slots, ws, stream) : launch_merge<__bf16>(p, slots, ws, stream);
+        return p.out == FA_F32 ? launch_d<f16_t, float>(pp, ws, stream) : launch_d<f16_t, _Float16>(pp, ws, stream);
+    return p.out == FA_F32 ? launch_d<bf16_t, float>(pp, ws, stream) : launch_d<bf16_t, __bf16>(pp, ws, stream);
 }
 
 }  // namespace fa

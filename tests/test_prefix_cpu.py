@@ -54,6 +54,7 @@ def test_workspace_sizes():
     assert need >= 2 * row and need % row == 0
     for Np, Nk in ((1, 1), (63, 1024), (4000, 17), (8191, 1000), (8192, 0)):
         assert 0 < prefix_workspace_bytes(64, 32, 8, 1, Np, Nk, 128, "bf16") <= need
+    assert prefix_workspace_bytes(64, 32, 8, 32, 8192, 1024, 128, "bf16") == 0   # one pass
     for over in (dict(B=0), dict(Hq=3, Hkv=2), dict(D=96), dict(Np=0), dict(Nk=-1), dict(Np=1 << 30), dict(in_dtype="f32"),
                  dict(B=1 << 30, Nq=1 << 30)):
         a = dict(B=2, Hq=4, Hkv=2, Nq=1, Np=100, Nk=100, D=64, in_dtype="f16")

@@ -1,8 +1,8 @@
 """fwd_prefix and fwd_prefix_paged against the definition in 64 bits on each
 sequence's prefix and suffix one after the other.
 
-Keys past a sequence's length hold NaN, the table's rows but the first name no
-page for the prefix, and a suffix page without valid keys is no page either.
+Keys past a sequence's length hold NaN, and the table's entry for a suffix page
+without valid keys is no page.
 The tolerance is that of the attention forward (helpers.check_against)."""
 import random
 
@@ -69,7 +69,7 @@ def check_case(B, Hq, Hkv, Nq, Np, Nk, D, dt, causal, lens, page, seed=7, scale=
                 pool[perm[np_:-1].long()] = suf.reshape(B * ns, page, Hkv, D)
             pools.append(pool.cuda())
         table = torch.full((B, np_ + ns), 1 << 30, dtype=torch.int32)
-        table[0, :np_] = perm[:np_]
+        table[:, :np_] = perm[:np_]
         for b in range(B):
             used = -(-max(total[b] - Np, 0) // page)
             table[b, np_:np_ + used] = perm[np_ + b * ns:np_ + b * ns + used]
@@ -109,6 +109,10 @@ EDGES = [
     (2, 4, 4, 64, 5120, 128, 128, "bf16", True, [5248, 5200], 64),
     (2, 4, 4, 64, 5120, 128, 128, "bf16", False, [5248, 5000], 64),
     (40, 4, 1, 3, 320, 64, 64, "bf16", True, [64 + 320 - 3 * i for i in range(40)], 64),
+    (2, 8, 2, 31, 90, 40, 64, "f16", True, [40, 20], 0),                  # either side of the rows from which one pass is taken
+    (2, 8, 2, 32, 90, 40, 64, "f16", True, [40, 20], 0),
+    (2, 8, 2, 31, 128, 64, 128, "bf16", True, [192, 100], 64),
+    (2, 8, 2, 32, 128, 64, 128, "bf16", True, [192, 100], 64),
     (2, 16, 2, 7, 500, 3, 64, "f16", True, [3, 1], 0),                    # fewer suffix rows than queries
 ]
 
