@@ -47,7 +47,7 @@ class _Runtime:
         self.int32 = torch.int32
         self.codes = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
         self.contiguous = torch.contiguous_format
-        self.current_device = torch.cuda.current_device
+        self.current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         self.stream = getattr(torch._C, "_cuda_getCurrentRawStream",
                               lambda index: torch.cuda.current_stream(index).cuda_stream)
 
@@ -216,7 +216,7 @@ def fwd_unfused(q, k, v, causal: bool = False, scale: float | None = None, out=N
 
 def _check_lengths(rt, seqlens_k, B, device):
     if (seqlens_k.dtype != rt.int32 or seqlens_k.shape != (B,) or not seqlens_k.is_contiguous()
-            or seqlens_k.device != device):
+            or seqlens_k.get_device() != device.index):
         raise ValueError("seqlens_k must be a contiguous int32 [B] tensor on q's device")
 
 
@@ -414,35 +414,35 @@ def _int32(n):
     return max(min(int(n), 0x7fffffff), -1)
 
 
-def _token_stride(t, name):
+def _token_stride(t, name, B, N, H, D):
     """Elements between the consecutive tokens of t [B, N, H, D], whose heads and
     columns are dense and whose sequences follow each other."""
-    B, N, H, D = t.shape
     sb, sn, sh, sd = t.stride()
-    step = sn if N > 1 else sb if B > 1 else H * D
-    if ((sd != 1 and D > 1) or (sh != D and H > 1) or (N > 1 and B > 1 and sb != N * sn) or step < H * D):
+    row = H * D
+    step = sn if N > 1 else sb if B > 1 else row
+    if ((sd != 1 and D > 1) or (sh != D and H > 1) or (N > 1 and B > 1 and sb != N * sn)
+            or step < row):   # (0, to the call, means dense)
         raise ValueError(f"{name} must be [B, N, H, D] with dense heads and one stride between its tokens")
     return step
 
 
-def _rotary(rt, inv_freq, positions, pair_axes, interleaved, B, N, device):
+def _rotary(rt, inv_freq, positions, pair_axes, interleaved, B, N, index):
     """The fa_rotary_t of a call (None: no rotation)."""
     if inv_freq is None:
         if positions is not None or pair_axes is not None:
             raise ValueError("positions and pair_axes need inv_freq")
         return None
     if (inv_freq.dtype != rt.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous()
-            or inv_freq.device != device):
+            or inv_freq.get_device() != index):
         raise ValueError("inv_freq must be a contiguous float32 [rot_dim / 2] tensor on k's device")
-    pairs, axes = inv_freq.shape[0], 1
-    r = _lib.Rotary(inv_freq.data_ptr(), None, 2 * pairs, 1 if interleaved else 0, 1)
+    pairs, axes, at = inv_freq.shape[0], 1, None
     if positions is not None:
         shape = tuple(positions.shape)
-        if (positions.dtype != rt.int32 or not positions.is_contiguous() or positions.device != device
+        if (positions.dtype != rt.int32 or not positions.is_contiguous() or positions.get_device() != index
                 or shape[-2:] != (B, N) or len(shape) > 3):
             raise ValueError("positions must be a contiguous int32 [B, N] or [axes, B, N] tensor on k's device")
-        axes = shape[0] if len(shape) == 3 else 1
-        r.positions, r.axes = positions.data_ptr(), axes
+        axes, at = shape[0] if len(shape) == 3 else 1, positions.data_ptr()
+    r = _lib.Rotary(inv_freq.data_ptr(), at, 2 * pairs, 1 if interleaved else 0, axes)
     if axes > 1:
         if pair_axes is None or len(pair_axes) != pairs:
             raise ValueError("several axes need pair_axes, the axis of each of the rot_dim / 2 pairs")
@@ -451,49 +451,57 @@ def _rotary(rt, inv_freq, positions, pair_axes, interleaved, B, N, device):
     return r
 
 
-def _append(k, v, k_cache, v_cache, block_table, seqlens_k, q, q_out, rotary):
+def _append(k, v, k_cache, v_cache, block_table, seqlens_k, q, q_out, inv_freq, positions, pair_axes, interleaved):
     lib = _lib.load()
-    rt = _runtime()
-    dt, dev = k.dtype, k.device
-    if not k.is_cuda or k.dim() != 4 or dt not in rt.codes:
+    rt = _RUNTIME or _runtime()
+    dt, index = k.dtype, k.get_device()
+    if index < 0 or k.dim() != 4 or dt not in rt.codes:
         raise ValueError("k must be a 4-D [B, N, Hkv, D] GPU tensor of float16, bfloat16 or float32")
-    if v.shape != k.shape or v.dtype != dt or v.device != dev:
+    shape, cshape = k.shape, k_cache.shape
+    if v.shape != shape or v.dtype != dt or v.get_device() != index:
         raise ValueError("v must have k's shape, dtype and device")
-    B, N, Hkv, D = k.shape
-    for name, t in (("k", k_cache), ("v", v_cache)):
-        if t.dim() != 4 or not t.is_contiguous() or t.dtype != dt or t.device != dev:
-            raise ValueError(f"the {name} cache must be contiguous and 4-D, of k's dtype and device")
-    first, rows, ch, cd = k_cache.shape
-    if v_cache.shape != k_cache.shape or ch != Hkv or cd != D or (block_table is None and first != B):
-        raise ValueError("the caches must have one shape, with k's heads and head size")
-    if (seqlens_k.dtype != rt.int32 or tuple(seqlens_k.shape) != (B,) or not seqlens_k.is_contiguous()
-            or seqlens_k.device != dev):
+    B, N, Hkv, D = shape
+    if (len(cshape) != 4 or v_cache.shape != cshape or not k_cache.is_contiguous() or not v_cache.is_contiguous()
+            or k_cache.dtype != dt or v_cache.dtype != dt or k_cache.get_device() != index
+            or v_cache.get_device() != index):
+        raise ValueError("the caches must be contiguous and 4-D, of one shape, and of k's dtype and device")
+    first, rows, ch, cd = cshape
+    if ch != Hkv or cd != D or (block_table is None and first != B):
+        raise ValueError("the caches must have k's heads and head size" + ("" if block_table is not None else " and batch"))
+    if (seqlens_k.dtype != rt.int32 or seqlens_k.shape != (B,) or not seqlens_k.is_contiguous()
+            or seqlens_k.get_device() != index):
         raise ValueError("seqlens_k must be a contiguous int32 [B] tensor on k's device")
-    Hq, qs = 0, 0
+    Hq = qs = 0
+    qp = qo = None
     if q is not None:
-        if q.dim() != 4 or q.dtype != dt or q.device != dev or q.shape[:2] != k.shape[:2] or q.shape[3] != D:
+        if q.dim() != 4 or q.dtype != dt or q.get_device() != index:
             raise ValueError("q must be [B, N, Hq, D] with k's B, N, D, dtype and device")
-        Hq, qs = q.shape[2], _token_stride(q, "q")
+        qb, qn, Hq, qd = q.shape
+        if qb != B or qn != N or qd != D:
+            raise ValueError("q must be [B, N, Hq, D] with k's B, N, D, dtype and device")
+        qs = _token_stride(q, "q", B, N, Hq, D)
         if q_out is None:
-            q_out = rt.torch.empty(q.shape, dtype=dt, device=dev)
-        elif q_out.shape != q.shape or q_out.dtype != dt or not q_out.is_contiguous() or q_out.device != dev:
+            q_out = _like(rt, q, dt)
+        elif q_out.shape != q.shape or q_out.dtype != dt or not q_out.is_contiguous() or q_out.get_device() != index:
             raise ValueError("q_out must be a contiguous tensor of q's shape, dtype and device")
+        qp, qo = q.data_ptr(), q_out.data_ptr()
     elif q_out is not None:
         raise ValueError("q_out needs q")
-    index = dev.index
-    ptrs = (k.data_ptr(), v.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
-            q.data_ptr() if q is not None else None, q_out.data_ptr() if q is not None else None, seqlens_k.data_ptr())
-    r = _rotary(rt, *rotary, B, N, dev)
-    tail = (qs, _token_stride(k, "k"), _token_stride(v, "v"), ctypes.addressof(r) if r is not None else None,
-            rt.stream(index), rt.codes[dt])
+    r = _rotary(rt, inv_freq, positions, pair_axes, interleaved, B, N, index)
+    ks, vs = _token_stride(k, "k", B, N, Hkv, D), _token_stride(v, "v", B, N, Hkv, D)
+    rp = None if r is None else ctypes.addressof(r)
     if block_table is None:
-        _call(rt, lib, index, lib.fa_kvcache_append, (*ptrs, B, Hq, Hkv, N, rows, D, *tail))
+        _call(rt, lib, index, lib.fa_kvcache_append,
+              (k.data_ptr(), v.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), qp, qo, seqlens_k.data_ptr(),
+               B, Hq, Hkv, N, rows, D, qs, ks, vs, rp, rt.stream(index), rt.codes[dt]))
     else:
         if (block_table.dtype != rt.int32 or block_table.dim() != 2 or block_table.shape[0] != B
-                or not block_table.is_contiguous() or block_table.device != dev):
+                or not block_table.is_contiguous() or block_table.get_device() != index):
             raise ValueError("block_table must be a contiguous int32 [B, max_pages] tensor on k's device")
         _call(rt, lib, index, lib.fa_kvcache_append_paged,
-              (*ptrs, block_table.data_ptr(), B, Hq, Hkv, N, D, rows, block_table.shape[1], first, *tail))
+              (k.data_ptr(), v.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), qp, qo, seqlens_k.data_ptr(),
+               block_table.data_ptr(), B, Hq, Hkv, N, D, rows, block_table.shape[1], first, qs, ks, vs, rp,
+               rt.stream(index), rt.codes[dt]))
     return q_out
 
 
@@ -514,7 +522,7 @@ def kvcache_append(k, v, k_cache, v_cache, seqlens_k, q=None, q_out=None, inv_fr
     sequence of ints); None: the cache rows.  Returns the rotated queries
     (``q_out`` if given, which may be ``q`` if that is contiguous; None without
     ``q``)."""
-    return _append(k, v, k_cache, v_cache, None, seqlens_k, q, q_out, (inv_freq, positions, pair_axes, interleaved))
+    return _append(k, v, k_cache, v_cache, None, seqlens_k, q, q_out, inv_freq, positions, pair_axes, interleaved)
 
 
 def kvcache_append_paged(k, v, k_pages, v_pages, block_table, seqlens_k, q=None, q_out=None, inv_freq=None,
@@ -525,8 +533,7 @@ def kvcache_append_paged(k, v, k_pages, v_pages, block_table, seqlens_k, q=None,
     (fa_kvcache_append_paged)."""
     if block_table is None:
         raise ValueError("block_table must be a contiguous int32 [B, max_pages] tensor on k's device")
-    return _append(k, v, k_pages, v_pages, block_table, seqlens_k, q, q_out,
-                   (inv_freq, positions, pair_axes, interleaved))
+    return _append(k, v, k_pages, v_pages, block_table, seqlens_k, q, q_out, inv_freq, positions, pair_axes, interleaved)
 
 
 def q8_0_gemv(w, x, out=None, out_dtype=None):

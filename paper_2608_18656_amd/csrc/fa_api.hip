@@ -125,10 +125,20 @@ struct Window {
     int size = 0, sinks = 0;
 };
 
-// Keys that a decode call with this window reads, at most.
-int decode_keys(int Nk, const Window &w) {
-    const long long n = (long long)w.size + w.sinks;
-    return w.size > 0 && n < Nk ? (int)n : Nk;
+// Splits of a decode call, and the most of any shorter cache.  With a window they
+// go by the keys that it leaves.  Up to ONE_SPLIT of those at D = 64 one split is as
+// quick as several and their merge, and saves the second launch (1028 keys, one
+// sequence, 32/8 heads: 10.3 us a call against 12.7 among others, 24.9 against 24.3
+// waited for; 2052 keys 16.8 against 12.8; D = 128, 516 keys 26.3 against 25.1 waited
+// for).
+constexpr int ONE_SPLIT = 1152;
+int decode_splits(int B, int Hq, int Hkv, int Nk, int D, const Window &w, bool most) {
+    long long keys = Nk;
+    if (w.size > 0) {
+        if ((long long)w.size + w.sinks < keys) keys = (long long)w.size + w.sinks;
+        if (D == 64 && keys <= ONE_SPLIT) return 1;
+    }
+    return most ? fa::decode_most_splits(B, Hq, Hkv, (int)keys, D) : fa::decode_default_splits(B, Hq, Hkv, (int)keys, D);
 }
 
 struct Paging {
@@ -156,8 +166,7 @@ fa_status_t run(const void *q, const void *k, const void *v, void *o, float *lse
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     hipError_t e;
     if (fa::decode_supported(Nq, Hkv, D, in)) {
-        const int keys = decode_keys(Nk, win);
-        const int S = splits_req > 0 ? splits_req : fa::decode_default_splits(B, Hq, Hkv, keys, D);
+        const int S = splits_req > 0 ? splits_req : decode_splits(B, Hq, Hkv, Nk, D, win, false);
         const size_t need = fa::decode_workspace_bytes(B, Hq, D, S);
         void *ws = nullptr;
         bool user = false;
@@ -168,7 +177,7 @@ fa_status_t run(const void *q, const void *k, const void *v, void *o, float *lse
             ws = cws->ptr;
             user = true;
         } else {
-            const int most = splits_req > 0 ? splits_req : fa::decode_most_splits(B, Hq, Hkv, keys, D);
+            const int most = splits_req > 0 ? splits_req : decode_splits(B, Hq, Hkv, Nk, D, win, true);
             st = get_workspace(need, fa::decode_workspace_bytes(B, Hq, D, most), s, &ws, &user);
             if (st != FA_OK) return st;
         }
@@ -552,8 +561,9 @@ fa_status_t fa_fwd_window_paged(const void *q, const void *k_pages, const void *
 
 size_t fa_window_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Nk, int D, int window, int sinks,
                                  fa_dtype_t in_dtype) {
-    if (window < 1 || sinks < 0 || Nk < 1) return 0;
-    return fa_workspace_bytes(B, Hq, Hkv, Nq, decode_keys(Nk, Window{window, sinks}), D, in_dtype, 0);
+    if (window < 1 || sinks < 0 || B < 1 || Hq < 1 || Hkv < 1 || Nk < 1 || Hq % Hkv != 0) return 0;
+    if (!fa::decode_supported(Nq, Hkv, D, in_dtype)) return 0;
+    return fa::decode_workspace_bytes(B, Hq, D, decode_splits(B, Hq, Hkv, Nk, D, Window{window, sinks}, true));
 }
 
 fa_status_t fa_fwd_prefix(const void *q, const void *k_prefix, const void *v_prefix, const void *k, const void *v,
