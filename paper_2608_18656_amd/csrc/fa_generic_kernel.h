@@ -55,6 +55,7 @@ namespace {
 
 constexpr int QB = 16;    // query columns per wave
 constexpr int CUS = 256;  // compute units of the card
+constexpr int SHORT_WINDOW = 512;   // keys up to which a window is short (launch_k)
 
 struct GenericArgs {
     const void *q, *k, *v;
@@ -638,6 +639,13 @@ hipError_t launch_t(const Problem &p, hipStream_t stream) {
 //     on; it loses where they are not (not causal, 300 to 390 workgroups, +13 to
 //     +26 %) and where a causal call's longest row block then decides (bf16, D =
 //     256, 32/8 x 1024 45.6 / 59.5, x 1371 80.6 / 77.3, x 1718 110 / 94)
+// With a window all rows but the first take about the same time, so that a causal
+// call's second half is no shorter, and a long chain of steps is rare:
+//   16 bits, (4, 2) past the line of (2, 4) at once: 16/2 x 1280 rows, window 300,
+//     D = 96 13.9 against 19.0 with (2, 2) and 23.0 with (2, 4)
+//   fp32 up to 128 columns, past the line of (1, 4): (2, 2) for windows of up to 512
+//     keys: 2 x 16/2 x 333, window 200, D = 96 24.1 / 29.7; 16 x 700, window 64, D =
+//     128 17.4 / 24.3; 16/2 x 1280, D = 64, window 500 34.6 / 34.1; D = 96, 1000 69 / 67
 // The lines are those of a whole card, so that a call's layout, and with it the
 // order of its sums, does not go by the device's mode.
 template <typename TIN, typename TOUT, int DP, bool WIN>
@@ -652,15 +660,18 @@ hipError_t launch_k(const Problem &p, hipStream_t s) {
     } else if constexpr (F32 || !WIDE) {
         constexpr int NS = F32 && !WIDE ? 1 : 2, KSP = WIDE ? 2 : 4;
         constexpr int FIT = 163840 / GCfg<TIN, DP, NS, KSP, NB>::BYTES;   // workgroups per CU by LDS
-        const int rounds = p.causal && p.Nk < 2LL * p.Nq ? 2 : 1;
+        const int rounds = !WIN && p.causal && p.Nk < 2LL * p.Nq ? 2 : 1;
         if (groups(NS) <= CUS * (FIT < 2 ? FIT : 2) * rounds) return launch_t<TIN, TOUT, DP, NS, KSP, NB, WIN>(p, s);
-        if constexpr (!F32 && DP == 96) {
+        if constexpr (!WIN && !F32 && DP == 96) {
             constexpr int FIT2 = 163840 / GCfg<TIN, DP, 2, 2, NB>::BYTES;
             if (rounds == 2 && groups(2) <= CUS * FIT2) return launch_t<TIN, TOUT, DP, 2, 2, NB, WIN>(p, s);
         }
     }
     if constexpr (WIDE && !PAIR) {
         if (groups(8) >= CUS) return launch_t<TIN, TOUT, DP, 8, 1, NB, WIN>(p, s);
+    }
+    if constexpr (WIN && F32 && !WIDE) {
+        if ((long long)p.window + p.sinks <= SHORT_WINDOW) return launch_t<TIN, TOUT, DP, 2, 2, NB, WIN>(p, s);
     }
     if constexpr (F32 && !WIDE) return launch_t<TIN, TOUT, DP, 2, 4, NB, WIN>(p, s);
     else if constexpr (!PAIR) return launch_t<TIN, TOUT, DP, 4, 2, NB, WIN>(p, s);

@@ -80,7 +80,7 @@ constexpr float kMaxLaneSum = 4096.0f;   // largest 16-weight lane sum kept with
 //           sequence's own keys, both a split of the keys.  The B Nq G rows of a
 //           key/value head are numbered together (token t, head e of the group:
 //           row t G + e).  Each leaves a partial result (accumulator, base, sum).
-//   JOIN    the shared keys, then the sequence's own
+//   JOIN    the shared keys, then the sequence's own (paged: the table has both)
 enum { ALL = 0, WINDOW = 1, PARTS = 2, JOIN = 3 };
 
 struct PrefillArgs {
@@ -173,7 +173,7 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
     constexpr int KSTEPS = D / 16;          // QK^T contraction steps
     constexpr int DT = D / 32;              // output column tiles
     constexpr int CPR = D / 8;              // 16-byte chunks per row
-    constexpr bool IN_BF16 = __is_same(TIN, bf16_t);
+    constexpr bool IN_BF16 = __is_same(TIN, bf16_t), SEGMENTS = MODE == JOIN && !PAGED;
 
     __shared__ __attribute__((aligned(1024))) unsigned short smem[SM::WORDS];
 
@@ -256,7 +256,7 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
     // PARTS: of the part: the prefix's or the sequence's own.  JOIN: of both.
     int valid = min(max(len, 0), a.Nk);
     if constexpr (MODE == PARTS) valid = own ? own_keys(a, b0) : a.prefix;
-    if constexpr (MODE == JOIN) valid = a.prefix + own_keys(a, b);
+    if constexpr (SEGMENTS) valid = a.prefix + own_keys(a, b);
     const int Nk = __builtin_amdgcn_readfirstlane(valid);
     const int off = Nk - Nq;
 
@@ -295,7 +295,7 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
         // some row does not see all of the part: every tile is masked
         if (__builtin_amdgcn_ballot_w64(rlim < Nk)) kfree_w = 0;
     }
-    if constexpr (MODE == JOIN) {
+    if constexpr (SEGMENTS) {
         near = (a.prefix + BC - 1) / BC;
         if (kend_wg > a.prefix) ntiles = near + (kend_wg - a.prefix + BC - 1) / BC;
     }
@@ -338,14 +338,20 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
         koff[j] = r * row_bytes + 16 * (c ^ kswz(r));
         voff[j] = r * row_bytes + 16 * (c ^ vswz(r));
     }
-    typedef uint4_t vregs_t[IN_BF16 ? NP : 1];
+    // WINDOW, PARTS: bf16 V also goes to LDS directly, as it is, and becomes fp16 in its
+    // place once it is there, so that no registers hold it during a step (window
+    // 1024, 32/8 heads, D = 128, bf16: 4096 rows 90.1 -> 85.1 us, 8192 168.6 -> 160.8; with
+    // five stages instead of three, and two waves per SIMD, 91.8 and 177.8; JOIN, 8 x
+    // 256 rows behind 4096 + 512 keys, 157.8 against 154.2 through registers).
+    constexpr bool RAW = IN_BF16 && (MODE == WINDOW || MODE == PARTS), VREG = IN_BF16 && !RAW;
+    typedef uint4_t vregs_t[VREG ? NP : 1];
     vregs_t vr;   // bf16: the next tile's V chunks, in flight during a step
     // Scalar state of the next tile to load: the address of its first key row
     // in K and V, which advances by one tile per load, and its number.  The
     // buffer view of a tile ends after its last valid key (keys past it read
     // as zero): a full tile's extent for the first Nk / BC tiles, then that of
     // the remaining keys, if any (one tile's extent fits 31 bits: tile_fits).
-    const bool prefix_first = MODE == JOIN || (MODE == PARTS && !own);   // the first tile is one of the prefix
+    const bool prefix_first = SEGMENTS || (MODE == PARTS && !own);   // the first tile is one of the prefix
     const size_t head0 = ((size_t)(MODE == PARTS ? b0 : b) * a.Nk * a.Hkv + g) * D;
     const S *kbase = reinterpret_cast<const S *>(prefix_first ? a.k_prefix : a.k);
     const S *vbase = reinterpret_cast<const S *>(prefix_first ? a.v_prefix : a.v);
@@ -353,8 +359,8 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
     const S *vtile = vbase + (PAGED ? 0 : prefix_first ? (size_t)g * D : head0);
     const int tile_bytes = (BC - 1) * row_bytes + D * (int)sizeof(S);
     auto bytes_of = [&](int rows) { return rows > 0 ? (rows - 1) * row_bytes + D * (int)sizeof(S) : 0; };
-    int full_tiles = MODE == JOIN ? a.prefix / BC : Nk / BC;
-    int last_bytes = bytes_of(MODE == JOIN ? a.prefix % BC : Nk % BC);
+    int full_tiles = SEGMENTS ? a.prefix / BC : Nk / BC;
+    int last_bytes = bytes_of(SEGMENTS ? a.prefix % BC : Nk % BC);
     int tload = 0;
     // paged K/V: the pool of pages, at head g.  Tiles are loaded in order
     // and a page holds a whole number of tiles, so the page index and the
@@ -400,7 +406,7 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
         if constexpr (MODE == WINDOW || MODE == PARTS) {
             if (gap > 0 && tload == near) go_to(near + gap);
         }
-        if constexpr (MODE == JOIN) {
+        if constexpr (SEGMENTS) {
             if (tload == near) {   // on to the sequence's own keys
                 ktile = reinterpret_cast<const S *>(a.k) + head0;
                 vtile = reinterpret_cast<const S *>(a.v) + head0;
@@ -450,7 +456,7 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
             const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<S *>(vtile), (short)0, nrec, 0x00020000);
 #pragma unroll
             for (int j = 0; j < NP; ++j) {
-                if constexpr (IN_BF16)
+                if constexpr (VREG)
                     vr[j] = __builtin_bit_cast(uint4_t, __builtin_amdgcn_raw_buffer_load_b128(rv, at(voff[j], j), 0, 0));
                 else
                     load_lds16(vtile, nrec, dst + 2 * SM::KSZ + 1024 * (NT / 64) * j, at(voff[j], j));
@@ -476,8 +482,10 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
         if constexpr (IN_BF16) {
             if (dov) {
 #pragma unroll
-                for (int j = 0; j < NP; ++j)
-                    st16(stage + SM::KSZ + 512 * (piece + (NT / 64) * j) + 8 * l, bf16x8_to_f16x8(vr[j]));
+                for (int j = 0; j < NP; ++j) {
+                    unsigned short *at = stage + SM::KSZ + 512 * (piece + (NT / 64) * j) + 8 * l;
+                    st16(at, bf16x8_to_f16x8(RAW ? ld16(at) : vr[j]));
+                }
             }
         }
     };
@@ -598,7 +606,7 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
     auto mask = [&](float16_t &s, int t) {
         int kw = t * BC + 32 * kh;        // first key of this wave's half
         int end = Nk;                     // keys from here on do not exist
-        if constexpr (MODE == JOIN) {
+        if constexpr (SEGMENTS) {
             if (t < near)
                 end = a.prefix;
             else
@@ -606,7 +614,7 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
         }
         // WINDOW: the last key that the slot's last row does not see any more
         const int passed = MODE == WINDOW ? row0 + WR - 1 + off - a.window : -1;
-        if (kw + 32 > (MODE == JOIN ? min(kfree_w, end) : kfree_w) || (MODE == WINDOW && kw <= passed && kw + 32 > a.sinks)) {
+        if (kw + 32 > (SEGMENTS ? min(kfree_w, end) : kfree_w) || (MODE == WINDOW && kw <= passed && kw + 32 > a.sinks)) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int key = kw + 8 * (r >> 2) + 4 * lh + (r & 3);
@@ -620,7 +628,9 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
 
     // p = 2^(s c + nbase) for the 16 scores of the lane, packed to f16 in the
     // key order of the two PV k-steps
-    float wsum = 0.f;   // all but ALL: the 16 weights' sum before they are rounded
+    // All but ALL: the 16 weights are summed before they are rounded, for a
+    // log-sum-exp of fp32 accuracy (2 to 3 % of JOIN's time, none of WINDOW's and PARTS')
+    float wsum = 0.f;
     auto exp_pack = [&](const float16_t &s, float nbase, half8_t &p0, half8_t &p1) {
         float p[16];
 #pragma unroll
@@ -690,11 +700,12 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
         vregs_t v0;
         gload_to(v0, 0);
         if (AHEAD == 2 && ntiles > 1) gload_to(vr, 1);
-        vstore_from(v0, stage_at(0));
+        if (!RAW) vstore_from(v0, stage_at(0));
         if (AHEAD == 2 && ntiles > 1)
             lds_loads_done<SM::SPLIT ? NP : 2 * NP>();   // all but those of tile 1
         else
             lds_loads_done<0>();
+        if (RAW) vstore_from(v0, stage_at(0));
     }
     lds_barrier();
     auto step = [&](int i, auto R) {   // R: stage of tile i (i % NSTAGE)

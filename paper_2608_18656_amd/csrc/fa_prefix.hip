@@ -11,7 +11,7 @@
 // into splits of the keys: the prefix's multiply while the others read.
 // Where a sequence's rows fill the 32 rows of a wave, the parts would share
 // nothing that the caches do not: then every row takes the prefix's keys and its
-// own in one pass (JOIN; paged caches: the paged prefill).
+// own in one pass (JOIN).
 #include <algorithm>
 
 #include "fa_checks.h"
@@ -177,12 +177,15 @@ hipError_t launch_join(const PrefixProblem &pp, hipStream_t stream) {
     if (nblocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
     a.nhg = Divisor(G / a.HW);
     a.per_mb = Divisor((unsigned)p.B * p.Hkv * (G / a.HW));
-    if (p.causal)
-        hipLaunchKernelGGL((prefill_kernel<TIN, TOUT, D, NSLOT, true, false, JOIN>), dim3((unsigned)nblocks),
-                           dim3(SM::NT), 0, stream, a);
+    const dim3 grid((unsigned)nblocks), block(SM::NT);
+    if (p.block_table && p.causal)
+        hipLaunchKernelGGL((prefill_kernel<TIN, TOUT, D, NSLOT, true, true, JOIN>), grid, block, 0, stream, a);
+    else if (p.block_table)
+        hipLaunchKernelGGL((prefill_kernel<TIN, TOUT, D, NSLOT, false, true, JOIN>), grid, block, 0, stream, a);
+    else if (p.causal)
+        hipLaunchKernelGGL((prefill_kernel<TIN, TOUT, D, NSLOT, true, false, JOIN>), grid, block, 0, stream, a);
     else
-        hipLaunchKernelGGL((prefill_kernel<TIN, TOUT, D, NSLOT, false, false, JOIN>), dim3((unsigned)nblocks),
-                           dim3(SM::NT), 0, stream, a);
+        hipLaunchKernelGGL((prefill_kernel<TIN, TOUT, D, NSLOT, false, false, JOIN>), grid, block, 0, stream, a);
     return hipGetLastError();
 }
 
@@ -221,7 +224,6 @@ size_t prefix_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Np, int Nk, in
 
 hipError_t launch_prefix(const PrefixProblem &pp, void *workspace, hipStream_t stream) {
     const Problem &p = pp.p;
-    if (p.block_table && one_pass(p.Nq)) return launch_prefill(p, stream);
     float *ws = reinterpret_cast<float *>(workspace);
     if (p.in == FA_F16)
         return p.out == FA_F32 ? launch_d<f16_t, float>(pp, ws, stream) : launch_d<f16_t, _Float16>(pp, ws, stream);
