@@ -142,11 +142,15 @@ __device__ __forceinline__ unsigned lds_address(void *p) {
 // which goes before the barrier that publishes the data.  base, bytes and dst
 // are wave-uniform; dst is an operand in m0, so that the compiler knows what m0
 // holds; the s_nop covers a scalar register that a vector instruction wrote
-// just before (five wait states to its use in an address).
-__device__ __forceinline__ void load_lds16(const void *base, int bytes, unsigned dst, int off) {
+// just before (five wait states to its use in an address).  NT: non-temporal, for
+// data that is read once.
+template <bool NT = false> __device__ __forceinline__ void load_lds16(const void *base, int bytes, unsigned dst, int off) {
     const unsigned long long p = (unsigned long long)base;   // below 2^48: the descriptor's stride bits stay 0
     const uint4_t rsrc = {(unsigned)p, (unsigned)(p >> 32), (unsigned)bytes, 0x00020000u};
-    asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(dst), "v"(off), "s"(rsrc) : "memory");
+    if constexpr (NT)
+        asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"{m0}"(dst), "v"(off), "s"(rsrc) : "memory");
+    else
+        asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(dst), "v"(off), "s"(rsrc) : "memory");
 }
 template <int N> __device__ __forceinline__ void lds_loads_done() {   // all but the last N loads of the wave
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");

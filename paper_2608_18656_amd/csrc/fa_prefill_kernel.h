@@ -447,21 +447,28 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
         };
         ++tload;
         const unsigned dst = lds0 + stage * (2 * SM::STAGE) + 1024 * piece;
-        if (dok) {
+        auto issue = [&](auto once) {   // once: nobody else reads these keys
+            constexpr bool ONCE = decltype(once)::value;
+            if (dok) {
 #pragma unroll
-            for (int j = 0; j < NP; ++j)
-                load_lds16(ktile, nrec, dst + 1024 * (NT / 64) * j, at(koff[j], j));
-        }
-        if (dov) {
-            const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<S *>(vtile), (short)0, nrec, 0x00020000);
-#pragma unroll
-            for (int j = 0; j < NP; ++j) {
-                if constexpr (VREG)
-                    vr[j] = __builtin_bit_cast(uint4_t, __builtin_amdgcn_raw_buffer_load_b128(rv, at(voff[j], j), 0, 0));
-                else
-                    load_lds16(vtile, nrec, dst + 2 * SM::KSZ + 1024 * (NT / 64) * j, at(voff[j], j));
+                for (int j = 0; j < NP; ++j)
+                    load_lds16<ONCE>(ktile, nrec, dst + 1024 * (NT / 64) * j, at(koff[j], j));
             }
-        }
+            if (dov) {
+                const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<S *>(vtile), (short)0, nrec, 0x00020000);
+#pragma unroll
+                for (int j = 0; j < NP; ++j) {
+                    if constexpr (VREG)
+                        vr[j] = __builtin_bit_cast(uint4_t, __builtin_amdgcn_raw_buffer_load_b128(rv, at(voff[j], j), 0, 0));
+                    else
+                        load_lds16<ONCE>(vtile, nrec, dst + 2 * SM::KSZ + 1024 * (NT / 64) * j, at(voff[j], j));
+                }
+            }
+        };
+        if (MODE == PARTS && own)
+            issue(std::true_type{});
+        else
+            issue(std::false_type{});
         ktile += BC * (size_t)row_elems;
         vtile += BC * (size_t)row_elems;
         if constexpr (PAGED) {
