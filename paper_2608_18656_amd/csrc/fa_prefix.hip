@@ -76,7 +76,14 @@ __global__ __launch_bounds__(256) void merge_kernel(const float *__restrict__ op
     }
 }
 
-// Splits of the prefix's keys and of a sequence's own.
+// Splits of the prefix's keys and of a sequence's own.  Both kinds of workgroups
+// take about the same number of tiles, so that all of them together fill the chip
+// once, but at least MIN_TILES; the prefix's, whose four slots all multiply, count
+// their tiles 5 / 4 at D = 128 (64 x 32/8 heads behind 8192 keys, 1024 to 64 of their
+// own: 48.6 us with 10 splits of the prefix, 46.3 with 12, 50.1 with 16).  More prefix
+// workgroups than one wave on every SIMD only leave more partial results: without
+// own keys, D = 128, 37.2 us with 43 splits (688 workgroups), 28.8 with 16 (256); D =
+// 64, 64 x 16/1 heads, 19.6 with 32, 18.4 with 16 (128 workgroups of eight waves).
 struct Plan {
     int prefix, own;
 };
@@ -90,13 +97,16 @@ Plan plan(int B, int Hq, int Hkv, int Nq, int Np, int Nk, int D, bool most) {
     const long long room = CUS * wpc;   // workgroups that the chip holds at once
     long long each = (pu * pt + su * st + room - 1) / room;
     if (each < MIN_TILES) each = MIN_TILES;
-    auto cut = [&](long long tiles, long long units) {
-        long long n = (tiles + each - 1) / each;
-        // (each >= units tiles / room, so n <= room / units + 1)
-        if (most) n = std::min((tiles + MIN_TILES - 1) / MIN_TILES, room / units + 1);
-        return n < 1 ? 1 : n > FA_MAX_SPLITS ? FA_MAX_SPLITS : (int)n;
-    };
-    return Plan{cut(pt, pu), Nk > 0 ? cut(st, su) : 0};
+    const long long weight = D == 64 ? 4 : 5;              // of a prefix tile, in quarters
+    const long long top = (D == 64 ? CUS / 2 : CUS) / pu;   // splits that give every SIMD one wave
+    auto least_tiles = [](long long tiles) { return (tiles + MIN_TILES - 1) / MIN_TILES; };
+    long long prefix = std::min(least_tiles(pt), top), own = std::min(least_tiles(st), room / su + 1);
+    if (!most) {
+        prefix = std::min(prefix, (pt * weight / 4 + each - 1) / each);
+        own = std::min(own, (st + each - 1) / each);   // (each >= su st / room)
+    }
+    auto count = [](long long n) { return n < 1 ? 1 : n > FA_MAX_SPLITS ? FA_MAX_SPLITS : (int)n; };
+    return Plan{count(prefix), Nk > 0 ? count(own) : 0};
 }
 
 // Rows of a sequence from which its own pass over all keys is taken.
