@@ -110,8 +110,8 @@ def _prepare(rt, q, k, v, out, lse, out_dtype, return_lse):
                 raise ValueError(f"{name} must be contiguous ([B, N, H, D] row-major)")
             if t.dim() != 4:
                 raise ValueError(f"{name} must be 4-D [B, N, H, D]")
-    dt, dev = q.dtype, q.device
-    if not (dev == k.device == v.device):
+    dt = q.dtype
+    if not (q.get_device() == k.get_device() == v.get_device()):
         raise ValueError("q, k, v must be on the same device")
     if not (dt == k.dtype == v.dtype) or dt not in rt.codes:
         raise ValueError("q, k, v must share one dtype among float16, bfloat16, float32")
@@ -253,8 +253,8 @@ def _prepare_paged(rt, q, k_pages, v_pages, block_table, seqlens_k, out, lse, ou
     for name, t in (("q", q), ("k_pages", k_pages), ("v_pages", v_pages)):
         if not t.is_cuda or not t.is_contiguous() or t.dim() != 4:
             raise ValueError(f"{name} must be a contiguous 4-D GPU tensor")
-    dt, dev = q.dtype, q.device
-    if not (dev == k_pages.device == v_pages.device):
+    dt, index = q.dtype, q.get_device()
+    if not (index == k_pages.get_device() == v_pages.get_device()):
         raise ValueError("q and the page pools must be on the same device")
     if not (dt == k_pages.dtype == v_pages.dtype) or dt not in rt.codes:
         raise ValueError("q and the page pools must share one dtype")
@@ -265,8 +265,8 @@ def _prepare_paged(rt, q, k_pages, v_pages, block_table, seqlens_k, out, lse, ou
     if Dk != D:
         raise ValueError("the page pools' head size differs from q's")
     for name, t in (("block_table", block_table), ("seqlens_k", seqlens_k)):
-        if (not t.is_cuda or t.dtype != rt.int32 or not t.is_contiguous() or t.device != dev
-                or (t is seqlens_k and tuple(t.shape) != (B,))):
+        if (t.dtype != rt.int32 or not t.is_contiguous() or t.get_device() != index
+                or (t is seqlens_k and t.shape != (B,))):
             raise ValueError(f"{name} must be a contiguous int32 tensor on q's device")
     if block_table.dim() != 2 or block_table.shape[0] != B:
         raise ValueError("block_table must be [B, max_pages]")
@@ -369,20 +369,20 @@ def fwd_prefix(q, k_prefix, v_prefix, k, v, seqlens_k=None, causal: bool = False
     lib = _lib.load()
     rt = _runtime()
     (B, Hq, Hkv, Nq, Nk, D), out, lse, odt = _prepare(rt, q, k, v, out, lse, out_dtype, return_lse)
-    if (k_prefix.dim() != 3 or k_prefix.shape != v_prefix.shape or k_prefix.shape[1:] != k.shape[2:]
-            or not k_prefix.is_contiguous() or not v_prefix.is_contiguous() or k_prefix.dtype != q.dtype
-            or v_prefix.dtype != q.dtype or k_prefix.device != q.device or v_prefix.device != q.device):
+    dt, index, shape = q.dtype, q.get_device(), k_prefix.shape
+    if (len(shape) != 3 or shape[1] != Hkv or shape[2] != D or v_prefix.shape != shape or not k_prefix.is_contiguous()
+            or not v_prefix.is_contiguous() or k_prefix.dtype != dt or v_prefix.dtype != dt
+            or k_prefix.get_device() != index or v_prefix.get_device() != index):
         raise ValueError("k_prefix and v_prefix must be contiguous [Np, Hkv, D] tensors of q's dtype and device")
     if seqlens_k is not None:
         _check_lengths(rt, seqlens_k, B, q.device)
     if scale is None:
         scale = 1.0 / math.sqrt(D)
-    index = q.device.index
     _call(rt, lib, index, lib.fa_fwd_prefix,
           (q.data_ptr(), k_prefix.data_ptr(), v_prefix.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
            lse.data_ptr() if lse is not None else None, seqlens_k.data_ptr() if seqlens_k is not None else None,
-           B, Hq, Hkv, Nq, k_prefix.shape[0], Nk, D, 1 if causal else 0, float(scale), rt.stream(index),
-           rt.codes[q.dtype], rt.codes.get(odt, -1),
+           B, Hq, Hkv, Nq, shape[0], Nk, D, 1 if causal else 0, float(scale), rt.stream(index), rt.codes[dt],
+           rt.codes.get(odt, -1),
            *((None, 0) if workspace is None else _workspace_arg(workspace, q.device))))
     return out, lse
 
