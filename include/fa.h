@@ -490,7 +490,7 @@ size_t fa_window_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Nk, int D, 
  * that sees none gives 0 and -inf).  fp16 / bf16 with D in {64, 128}.
  * workspace, workspace_bytes: device scratch of this call
  * (fa_prefix_workspace_bytes), 16-byte aligned, or NULL and 0: the library's or
- * the one that is set (see the top); calls that need none (Nq >= 32) ignore it.  Graphs that may run at the same time need
+ * the one that is set (see the top); calls that need none ignore it.  Graphs that may run at the same time need
  * workspaces of their own.
  * Errors: FA_ERR_NULL for a NULL tensor (or workspace with a size), FA_ERR_DIM
  * for a size < 1, Np + Nk above FA_MAX_PREFIX_KEYS, B * Nq * Hq above 2^31 - 1 or
@@ -518,8 +518,8 @@ fa_status_t fa_fwd_prefix_paged(const void *q, const void *k_pages, const void *
                                 void *stream, fa_dtype_t in_dtype, fa_dtype_t out_dtype,
                                 void *workspace, size_t workspace_bytes);
 
-/* Bytes of workspace that fa_fwd_prefix needs (0: none, or sizes it refuses); serves
- * every shorter prefix and suffix as well. */
+/* Bytes of workspace that fa_fwd_prefix needs with these sizes and with any shorter
+ * prefix and suffix (0: none, or sizes it refuses). */
 size_t fa_prefix_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Np, int Nk, int D,
                                  fa_dtype_t in_dtype);
 

@@ -9,9 +9,8 @@
 //   merge   the parts by their bases, the final normalisation, the log-sum-exp
 // Prefix and own parts are workgroups of one launch (prefill kernel, PARTS), cut
 // into splits of the keys: the prefix's multiply while the others read.
-// Where a sequence's rows fill the 32 rows of a wave, the parts would share
-// nothing that the caches do not: then every row takes the prefix's keys and its
-// own in one pass (JOIN).
+// Where there are rows enough for full waves on a full chip, or few keys, every
+// row takes the prefix's keys and its own in one pass (JOIN).
 #include <algorithm>
 
 #include "fa_checks.h"
@@ -76,27 +75,45 @@ __global__ __launch_bounds__(256) void merge_kernel(const float *__restrict__ op
     }
 }
 
-// Splits of the prefix's keys and of a sequence's own.  Both kinds of workgroups
-// take about the same number of tiles, so that all of them together fill the chip
-// once, but at least MIN_TILES; the prefix's, whose four slots all multiply, count
-// their tiles 5 / 4 at D = 128 (64 x 32/8 heads behind 8192 keys, 1024 to 64 of their
-// own: 48.6 us with 10 splits of the prefix, 46.3 with 12, 50.1 with 16).  More prefix
-// workgroups than one wave on every SIMD only leave more partial results: without
-// own keys, D = 128, 37.2 us with 43 splits (688 workgroups), 28.8 with 16 (256); D =
-// 64, 64 x 16/1 heads, 19.6 with 32, 18.4 with 16 (128 workgroups of eight waves).
+// Parts or one pass, and the splits.
+//
+// Parts: splits of the prefix's keys and of a sequence's own.  Both kinds of
+// workgroups take about the same number of tiles, so that all of them together
+// fill the chip once, but at least MIN_TILES; the prefix's, whose four slots all
+// multiply, count their tiles 5 / 4 at D = 128 (64 x 32/8 heads behind 8192 keys, 1024
+// to 64 of their own: 48.6 us with 10 splits of the prefix, 46.3 with 12, 50.1 with
+// 16).  More prefix workgroups than one wave on every SIMD only leave more partial
+// results: without own keys, D = 128, 37.2 us with 43 splits (688 workgroups), 28.8
+// with 16 (256); D = 64, 64 x 16/1 heads, 19.6 with 32, 18.4 with 16 (128 workgroups
+// of eight waves).
+//
+// One pass has no partial results and no merge, but no splits either, and pads
+// each sequence's rows to 32.  Both times are estimated from the tiles (us a
+// tile with one, two and three workgroups on a CU, D = 128: 0.72, 1.13, 1.56; D = 64,
+// two at most: 0.65, 1.0), a start and end, and the partial results' traffic at 5
+// bytes a ns.  Over 55 calls of 1 to 128 rows the choice was the quicker one (us, one
+// pass / parts; 32/8 heads, D = 128: 8 x 48 rows behind 4096 keys 96 / 65, x 128 98 /
+// 123, 32 x 8 behind 1000 32 / 24, x 24 33 / 45; 2 x 48 behind 8000 184 / 35; 16 x 8,
+// 32/4 heads, D = 64, behind 500 11 / 14).
 struct Plan {
-    int prefix, own;
+    int prefix, own;   // 0, 0: one pass
 };
+
+// Query heads per workgroup in one pass.
+int pass_heads(int G) { return G % 4 == 0 ? 4 : G % 2 == 0 ? 2 : 1; }
 
 // most: at least as many of both as any shorter prefix and suffix get.
 Plan plan(int B, int Hq, int Hkv, int Nq, int Np, int Nk, int D, bool most) {
     const int BC = D == 64 ? Cfg<64>::BC : Cfg<128>::BC, wpc = D == 64 ? Cfg<64>::WPC : Cfg<128>::WPC;
     const long long G = Hq / Hkv, rows = B * G * Nq;
-    const long long pu = (rows + ROWS - 1) / ROWS * Hkv, pt = (Np + BC - 1) / BC;
-    const long long su = (G * Nq + ROWS - 1) / ROWS * Hkv * B, st = (Nk + BC - 1) / BC;
+    const long long pu = (rows + ROWS - 1) / ROWS * Hkv, pt = ((long long)Np + BC - 1) / BC;
+    const long long su = (G * Nq + ROWS - 1) / ROWS * Hkv * B, st = ((long long)Nk + BC - 1) / BC;
     const long long room = CUS * wpc;   // workgroups that the chip holds at once
-    long long each = (pu * pt + su * st + room - 1) / room;
-    if (each < MIN_TILES) each = MIN_TILES;
+    const int hw = pass_heads((int)G), pass_rows = WR * NSLOT / hw;
+    const long long passes = ((long long)Nq + pass_rows - 1) / pass_rows * B * Hkv * (G / hw);
+    if (Nq >= WR && passes >= room) return Plan{0, 0};   // full waves on a full chip
+
+    const long long each = std::max((long long)MIN_TILES, (pu * pt + su * st + room - 1) / room);
     const long long weight = D == 64 ? 4 : 5;              // of a prefix tile, in quarters
     const long long top = (D == 64 ? CUS / 2 : CUS) / pu;   // splits that give every SIMD one wave
     auto least_tiles = [](long long tiles) { return (tiles + MIN_TILES - 1) / MIN_TILES; };
@@ -106,11 +123,18 @@ Plan plan(int B, int Hq, int Hkv, int Nq, int Np, int Nk, int D, bool most) {
         own = std::min(own, (st + each - 1) / each);   // (each >= su st / room)
     }
     auto count = [](long long n) { return n < 1 ? 1 : n > FA_MAX_SPLITS ? FA_MAX_SPLITS : (int)n; };
-    return Plan{count(prefix), Nk > 0 ? count(own) : 0};
-}
+    const Plan parts{count(prefix), Nk > 0 ? count(own) : 0};
+    if (most) return parts;
 
-// Rows of a sequence from which its own pass over all keys is taken.
-bool one_pass(int Nq) { return Nq >= WR; }
+    const long long tile128[] = {0, 720, 1130, 1560}, tile64[] = {0, 650, 1000};   // ns, by workgroups on the CU
+    const long long *tile = D == 64 ? tile64 : tile128;
+    const long long rest = (passes % room + CUS - 1) / CUS;
+    const long long pass_ns = 5000 + (pt + st) * (passes / room * tile[wpc] + tile[rest]);
+    const long long longest = std::max((pt + parts.prefix - 1) / parts.prefix, parts.own ? (st + parts.own - 1) / parts.own : 0);
+    const long long parts_ns = 11000 + std::max(longest * tile[1], (pu * pt + su * st) * tile[wpc] / room) +
+                               rows * Hkv * (parts.prefix + parts.own) * (D + 2) * 8 / 5000;
+    return pass_ns < parts_ns ? Plan{0, 0} : parts;
+}
 
 void common_args(const PrefixProblem &pp, PrefillArgs &a) {
     const Problem &p = pp.p;
@@ -179,7 +203,7 @@ hipError_t launch_join(const PrefixProblem &pp, hipStream_t stream) {
     PrefillArgs a;
     common_args(pp, a);
     const int G = a.G;
-    a.HW = G % 4 == 0 ? 4 : G % 2 == 0 ? 2 : 1;
+    a.HW = pass_heads(G);
     a.lgHW = a.HW == 4 ? 2 : a.HW == 2 ? 1 : 0;
     const int RB = NSLOT / a.HW;
     a.nmb = a.first = (p.Nq + WR * RB - 1) / (WR * RB);
@@ -217,9 +241,9 @@ hipError_t launch_merge(const Problem &p, int slots, const float *ws, hipStream_
 template <typename TIN, typename TOUT>
 hipError_t launch_d(const PrefixProblem &pp, float *ws, hipStream_t stream) {
     const Problem &p = pp.p;
-    if (one_pass(p.Nq))
-        return p.D == 64 ? launch_join<TIN, TOUT, 64>(pp, stream) : launch_join<TIN, TOUT, 128>(pp, stream);
     const Plan n = plan(p.B, p.Hq, p.Hkv, p.Nq, pp.Np, pp.own, p.D, false);
+    if (n.prefix == 0)
+        return p.D == 64 ? launch_join<TIN, TOUT, 64>(pp, stream) : launch_join<TIN, TOUT, 128>(pp, stream);
     const hipError_t e = p.D == 64 ? launch_parts<TIN, 64>(pp, n, ws, stream) : launch_parts<TIN, 128>(pp, n, ws, stream);
     return e != hipSuccess ? e : launch_merge<TOUT>(p, n.prefix + n.own, ws, stream);
 }
@@ -227,7 +251,6 @@ hipError_t launch_d(const PrefixProblem &pp, float *ws, hipStream_t stream) {
 }  // namespace
 
 size_t prefix_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Np, int Nk, int D, bool most) {
-    if (one_pass(Nq)) return 0;
     const Plan n = plan(B, Hq, Hkv, Nq, Np, Nk, D, most);
     return (size_t)B * Nq * Hq * (n.prefix + n.own) * (size_t)(D + 2) * sizeof(float);
 }

@@ -6,7 +6,7 @@ from paper_2608_18656_amd import _lib, prefix_workspace_bytes
 
 M = 1 << 24
 GOOD = dict(q=M, kp=2 * M, vp=3 * M, k=4 * M, v=5 * M, o=6 * M, lse=7 * M, lens=8 * M, table=9 * M, B=2, Hq=4, Hkv=2, Nq=1,
-            Np=128, Nk=64, D=64, ps=64, mp=3, np=8, pl=128, causal=1, scale=0.125, it=0, ot=0, ws=10 * M, wb=1 << 22)
+            Np=8000, Nk=64, D=64, ps=64, mp=126, np=200, pl=8000, causal=1, scale=0.125, it=0, ot=0, ws=10 * M, wb=1 << 22)
 
 
 def prefix(paged, **over):
@@ -23,7 +23,7 @@ def prefix(paged, **over):
 @pytest.mark.parametrize("paged", [False, True])
 @pytest.mark.parametrize("over,code", [
     ({"q": None}, 1), ({"k": None}, 1), ({"o": None}, 1), ({"B": 0}, 2), ({"Nq": 0}, 2), ({"Hq": 3}, 3),
-    ({"D": 60}, 4), ({"D": 96}, 4), ({"Nq": 193}, 5), ({"scale": float("nan")}, 6), ({"v": 5 * M + 8}, 7),
+    ({"D": 60}, 4), ({"D": 96}, 4), ({"Nq": 8065}, 5), ({"scale": float("nan")}, 6), ({"v": 5 * M + 8}, 7),
     ({"lens": 8 * M + 2}, 7), ({"o": M}, 8), ({"o": 8 * M}, 8), ({"lse": 6 * M}, 8), ({"lse": 4 * M}, 8), ({"it": 3}, 9),
     ({"ot": 1}, 9), ({"it": 2, "ot": 2}, 9), ({"B": 1 << 20, "Nq": 1 << 12, "causal": 0}, 2),
     ({"ws": None}, 1), ({"ws": 10 * M + 8}, 7), ({"wb": 64}, 10), ({"ws": 6 * M}, 8), ({"ws": 5 * M}, 8), ({"ws": 8 * M}, 8),
@@ -42,7 +42,7 @@ def test_refusals_contiguous(over, code):
 
 @pytest.mark.parametrize("over,code", [
     ({"table": None}, 1), ({"lens": None}, 1), ({"ps": 96}, 2), ({"mp": 0}, 2), ({"np": 0}, 2), ({"pl": 0}, 2),
-    ({"pl": 100}, 2), ({"pl": 256}, 2), ({"pl": -64}, 2), ({"table": 9 * M + 2}, 7), ({"table": 6 * M}, 8), ({"ws": 9 * M}, 8),
+    ({"pl": 100}, 2), ({"pl": 64 * 127}, 2), ({"pl": -64}, 2), ({"table": 9 * M + 2}, 7), ({"table": 6 * M}, 8), ({"ws": 9 * M}, 8),
 ])
 def test_refusals_paged(over, code):
     assert prefix(True, **over) == code
@@ -54,7 +54,7 @@ def test_workspace_sizes():
     assert need >= 2 * row and need % row == 0
     for Np, Nk in ((1, 1), (63, 1024), (4000, 17), (8191, 1000), (8192, 0)):
         assert 0 < prefix_workspace_bytes(64, 32, 8, 1, Np, Nk, 128, "bf16") <= need
-    assert prefix_workspace_bytes(64, 32, 8, 32, 8192, 1024, 128, "bf16") == 0   # one pass
+    assert prefix_workspace_bytes(64, 32, 8, 64, 8192, 1024, 128, "bf16") == 0   # full waves on a full chip: one pass
     for over in (dict(B=0), dict(Hq=3, Hkv=2), dict(D=96), dict(Np=0), dict(Nk=-1), dict(Np=1 << 30), dict(in_dtype="f32"),
                  dict(B=1 << 30, Nq=1 << 30)):
         a = dict(B=2, Hq=4, Hkv=2, Nq=1, Np=100, Nk=100, D=64, in_dtype="f16")

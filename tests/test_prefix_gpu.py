@@ -109,8 +109,13 @@ EDGES = [
     (2, 4, 4, 64, 5120, 128, 128, "bf16", True, [5248, 5200], 64),
     (2, 4, 4, 64, 5120, 128, 128, "bf16", False, [5248, 5000], 64),
     (40, 4, 1, 3, 320, 64, 64, "bf16", True, [64 + 320 - 3 * i for i in range(40)], 64),
-    (2, 8, 2, 31, 90, 40, 64, "f16", True, [40, 20], 0),                  # either side of the rows from which one pass is taken
+    (2, 8, 2, 31, 90, 40, 64, "f16", True, [40, 20], 0),                  # one pass: few keys
     (2, 8, 2, 32, 90, 40, 64, "f16", True, [40, 20], 0),
+    (2, 8, 2, 32, 2500, 90, 64, "f16", True, [90, 20], 0),                # parts, full waves
+    (40, 8, 4, 260, 90, 300, 64, "f16", True, [300 - 7 * i for i in range(40)], 0),    # one pass: full chip
+    (24, 8, 8, 300, 200, 320, 128, "bf16", True, [320 - 13 * i for i in range(24)], 0),
+    (12, 3, 1, 1, 30, 9, 128, "bf16", True, list(range(10)) + [9, 9], 0),  # one pass, one row
+    (12, 16, 1, 1, 64, 64, 64, "bf16", False, [64 + 5 * i for i in range(12)], 64),
     (2, 8, 2, 31, 128, 64, 128, "bf16", True, [192, 100], 64),
     (2, 8, 2, 32, 128, 64, 128, "bf16", True, [192, 100], 64),
     (2, 16, 2, 7, 500, 3, 64, "f16", True, [3, 1], 0),                    # fewer suffix rows than queries
