@@ -450,10 +450,10 @@ fa_status_t fa_kvcache_append_paged(const void *k, const void *v, void *k_pages,
  * call's sequence sees (between the sinks and the first query's window, or past
  * the length) may hold anything, also infinities and NaN; keys that some do see
  * must be finite, since a weight of 0 times an infinite value is NaN.
- * workspace, workspace_bytes: this call's own decode workspace
- * (fa_window_workspace_bytes; used with Nq = 1 as fa_fwd_ws does), or NULL and 0:
- * the library's or the one that is set.  Graphs that may run at the same time
- * need workspaces of their own.
+ * workspace, workspace_bytes: this call's own scratch for partial results
+ * (fa_window_workspace_bytes, 16-byte aligned; calls that need none ignore it), or
+ * NULL and 0: the library's or the one that is set (see the top).  Graphs that may
+ * run at the same time need workspaces of their own.
  * Errors: FA_ERR_WINDOW for window < 1 or sinks < 0; otherwise those of
  * fa_fwd_kvcache_ws (of fa_fwd_kvcache without a workspace). */
 fa_status_t fa_fwd_window(const void *q, const void *k, const void *v, void *o, float *lse,
@@ -472,9 +472,8 @@ fa_status_t fa_fwd_window_paged(const void *q, const void *k_pages, const void *
                                 fa_dtype_t in_dtype, fa_dtype_t out_dtype, void *workspace,
                                 size_t workspace_bytes);
 
-/* Bytes of decode workspace that fa_fwd_window (Nk = page_size * max_pages for
- * the paged form) needs: 0 when the call takes no split-KV path.  The size
- * serves shorter caches as well. */
+/* Bytes of workspace that fa_fwd_window (Nk = page_size * max_pages for the paged
+ * form) needs with these sizes and with any shorter cache (0: none). */
 size_t fa_window_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Nk, int D, int window,
                                  int sinks, fa_dtype_t in_dtype);
 

@@ -302,7 +302,7 @@ def fwd_kvcache_paged(q, k_pages, v_pages, block_table, seqlens_k, causal: bool 
 
 
 def window_workspace_bytes(B, Hq, Hkv, Nq, Nk, D, window, in_dtype: str, sinks: int = 0) -> int:
-    """Decode workspace bytes of fwd_window (fa_window_workspace_bytes)."""
+    """Workspace bytes of fwd_window (fa_window_workspace_bytes)."""
     return int(_lib.load().fa_window_workspace_bytes(B, Hq, Hkv, Nq, Nk, D, _int32(window), _int32(sinks),
                                                      DTYPE_CODES[in_dtype]))
 
@@ -314,7 +314,7 @@ def fwd_window(q, k, v, window: int, sinks: int = 0, seqlens_k=None, scale: floa
     (fa_fwd_window).  q [B, Nq, Hq, D] holds the last Nq of each sequence's
     ``seqlens_k`` (int32 [B]; None: Nk) keys in k, v [B, Nk, Hkv, D]: a whole
     prompt, a chunk of one, or one token.  Rows that see no key give 0 and lse
-    -inf.  ``workspace``: this call's own decode workspace (uint8 GPU tensor of
+    -inf.  ``workspace``: this call's own scratch (uint8 GPU tensor of
     window_workspace_bytes(...) bytes).  Returns (out, lse) as ``fwd``."""
     lib = _lib.load()
     rt = _runtime()

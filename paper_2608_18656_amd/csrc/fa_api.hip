@@ -164,11 +164,21 @@ fa_status_t run(const void *q, const void *k, const void *v, void *o, float *lse
                   pg.block_table, pg.page_size, pg.max_pages, pg.num_pages,
                   win.size < Nk ? win.size : Nk, win.sinks < Nk ? win.sinks : Nk};
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    hipError_t e;
-    if (fa::decode_supported(Nq, Hkv, D, in)) {
-        const int S = splits_req > 0 ? splits_req : decode_splits(B, Hq, Hkv, Nk, D, win, false);
-        const size_t need = fa::decode_workspace_bytes(B, Hq, D, S);
-        void *ws = nullptr;
+    const bool decode = fa::decode_supported(Nq, Hkv, D, in), prefill = fa::prefill_supported(Hkv, D, in);
+    const bool windowed = win.size > 0;
+    // partial results: bytes that the call uses, and that a new buffer holds
+    int S = 1;
+    size_t need = 0, room = 0;
+    if (decode) {
+        S = splits_req > 0 ? splits_req : decode_splits(B, Hq, Hkv, Nk, D, win, false);
+        need = fa::decode_workspace_bytes(B, Hq, D, S);
+        room = fa::decode_workspace_bytes(B, Hq, D, splits_req > 0 ? splits_req : decode_splits(B, Hq, Hkv, Nk, D, win, true));
+    } else if (windowed && prefill) {
+        need = fa::window_workspace_bytes(B, Hq, Hkv, Nq, Nk, D, p.window, p.sinks, false);
+        room = fa::window_workspace_bytes(B, Hq, Hkv, Nq, Nk, D, p.window, p.sinks, true);
+    }
+    void *ws = nullptr;
+    if (need > 0) {
         bool user = false;
         if (cws) {   // this call's own workspace: checked here, never allocated
             if (!cws->ptr) return FA_ERR_NULL;
@@ -177,8 +187,7 @@ fa_status_t run(const void *q, const void *k, const void *v, void *o, float *lse
             ws = cws->ptr;
             user = true;
         } else {
-            const int most = splits_req > 0 ? splits_req : decode_splits(B, Hq, Hkv, Nk, D, win, true);
-            st = get_workspace(need, fa::decode_workspace_bytes(B, Hq, D, most), s, &ws, &user);
+            st = get_workspace(need, room, s, &ws, &user);
             if (st != FA_OK) return st;
         }
         if (user) {   // a caller-owned workspace must not overlap the call's tensors
@@ -189,12 +198,10 @@ fa_status_t run(const void *q, const void *k, const void *v, void *o, float *lse
                 overlaps(ws, need, o, ob) || (lse && overlaps(ws, need, lse, lb)))
                 return FA_ERR_ALIAS;
         }
-        e = fa::launch_decode(p, S, ws, s);
-    } else if (fa::prefill_supported(Hkv, D, in)) {
-        e = win.size > 0 ? fa::launch_prefill_window(p, s) : fa::launch_prefill(p, s);
-    } else {
-        e = win.size > 0 ? fa::launch_generic_window(p, s) : fa::launch_generic(p, s);
     }
+    const hipError_t e = decode ? fa::launch_decode(p, S, ws, s)
+                         : prefill ? (windowed ? fa::launch_prefill_window(p, ws, s) : fa::launch_prefill(p, s))
+                                   : (windowed ? fa::launch_generic_window(p, s) : fa::launch_generic(p, s));
     return e == hipSuccess ? FA_OK : FA_ERR_HIP;
 }
 
@@ -562,8 +569,10 @@ fa_status_t fa_fwd_window_paged(const void *q, const void *k_pages, const void *
 size_t fa_window_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Nk, int D, int window, int sinks,
                                  fa_dtype_t in_dtype) {
     if (window < 1 || sinks < 0 || B < 1 || Hq < 1 || Hkv < 1 || Nk < 1 || Hq % Hkv != 0) return 0;
-    if (!fa::decode_supported(Nq, Hkv, D, in_dtype)) return 0;
-    return fa::decode_workspace_bytes(B, Hq, D, decode_splits(B, Hq, Hkv, Nk, D, Window{window, sinks}, true));
+    if (fa::decode_supported(Nq, Hkv, D, in_dtype))
+        return fa::decode_workspace_bytes(B, Hq, D, decode_splits(B, Hq, Hkv, Nk, D, Window{window, sinks}, true));
+    return Nq >= 1 && fa::prefill_supported(Hkv, D, in_dtype)
+               ? fa::window_workspace_bytes(B, Hq, Hkv, Nq, Nk, D, window, sinks, true) : 0;
 }
 
 fa_status_t fa_fwd_prefix(const void *q, const void *k_prefix, const void *v_prefix, const void *k, const void *v,

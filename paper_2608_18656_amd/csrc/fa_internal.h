@@ -57,7 +57,9 @@ struct AppendProblem {
 // Each launcher enqueues its kernels on `stream` and returns the first HIP
 // error (hipSuccess when the launch was accepted).
 hipError_t launch_prefill(const Problem &p, hipStream_t stream);
-hipError_t launch_prefill_window(const Problem &p, hipStream_t stream);
+hipError_t launch_prefill_window(const Problem &p, void *workspace, hipStream_t stream);
+// out and lse from `slots` partial results a row: accumulators [B Nq][Hq][slots][D], bases and sums.
+hipError_t launch_merge(const Problem &p, int slots, const float *workspace, hipStream_t stream);
 hipError_t launch_generic(const Problem &p, hipStream_t stream);
 hipError_t launch_generic_window(const Problem &p, hipStream_t stream);
 hipError_t launch_decode(const Problem &p, int splits, void *workspace, hipStream_t stream);
@@ -76,6 +78,9 @@ size_t decode_workspace_bytes(int B, int Hq, int D, int splits);
 
 // Partial results of prefix and suffix (0: one pass); most: enough for every shorter one as well.
 size_t prefix_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Np, int Nk, int D, bool most);
+
+// Partial results of a window's row blocks (0: none); most: enough for every shorter cache as well.
+size_t window_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Nk, int D, int window, int sinks, bool most);
 
 // Unfused path: supported shapes and the workspace it needs (0 when a size is
 // < 1 or the product overflows).

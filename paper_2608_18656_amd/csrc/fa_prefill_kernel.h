@@ -81,7 +81,9 @@ constexpr float kMaxLaneSum = 4096.0f;   // largest 16-weight lane sum kept with
 //           key/value head are numbered together (token t, head e of the group:
 //           row t G + e).  Each leaves a partial result (accumulator, base, sum).
 //   JOIN    the shared keys, then the sequence's own (paged: the table has both)
-enum { ALL = 0, WINDOW = 1, PARTS = 2, JOIN = 3 };
+//   WINDOW_PARTS  WINDOW with each row block's tiles split over workgroups, which
+//           leave partial results
+enum { ALL = 0, WINDOW = 1, PARTS = 2, JOIN = 3, WINDOW_PARTS = 4 };
 
 struct PrefillArgs {
     const void *q, *k, *v;
@@ -106,7 +108,7 @@ struct PrefillArgs {
     int page_size, max_pages, num_pages;
     // all but ALL
     Divisor page_div;     // page_size
-    int window, sinks;    // WINDOW: at most Nk each
+    int window, sinks;    // WINDOW, WINDOW_PARTS: at most Nk each
     // PARTS, JOIN: k, v and Nk are the sequences' own keys (paged: of all)
     const void *k_prefix, *v_prefix;
     int prefix;           // keys of the prefix
@@ -116,9 +118,11 @@ struct PrefillArgs {
     int first_page;       // table entry of a sequence's own first page
     int causal, rows;     // rows: B Nq G
     int prefix_blocks;    // workgroups of the prefix, ahead of the others
-    Divisor splits, own_splits;   // of the prefix's keys and of a sequence's own
+    Divisor own_splits;   // of a sequence's own keys
     Divisor batch, tokens, group;   // B, Nq, G
-    float *opart, *mpart, *lpart;   // [token][head][slots] partial results: the prefix's, then the own ones
+    // PARTS, WINDOW_PARTS
+    Divisor splits;       // of the prefix's keys, of a row block's tiles
+    float *opart, *mpart, *lpart;   // [token][head][slots] partial results (PARTS: the prefix's, then the own ones)
     int slots;
 };
 
@@ -174,6 +178,7 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
     constexpr int DT = D / 32;              // output column tiles
     constexpr int CPR = D / 8;              // 16-byte chunks per row
     constexpr bool IN_BF16 = __is_same(TIN, bf16_t), SEGMENTS = MODE == JOIN && !PAGED;
+    constexpr bool WIN = MODE == WINDOW || MODE == WINDOW_PARTS, JUMPS = WIN || MODE == PARTS;   // JUMPS: not all tiles are visited
 
     __shared__ __attribute__((aligned(1024))) unsigned short smem[SM::WORDS];
 
@@ -182,7 +187,8 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
     const int l = tid & 63, lq = l & 31, lh = l >> 5;
     const int kh = w / NSLOT, slot = w % NSLOT;   // kh: the wave's 32 keys of a tile
     const int RB = NSLOT >> a.lgHW;
-    const int bid = blockIdx.x;
+    const int wg = blockIdx.x;
+    const int bid = MODE == WINDOW_PARTS ? (int)a.splits.div(wg) : wg;
     // Row block of this workgroup.  Latest rows (most keys) first, so that
     // the short causal blocks fill the tail; when the whole grid is resident
     // at once, only one workgroup for every CU in that order and the others
@@ -273,11 +279,18 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
     // JOIN: the prefix's tiles are the first `near`, the own ones follow.
     int near = 0, gap = 0, first_key = 0;
     int rlim = 0;   // PARTS: keys of the part that the lane's row sees
-    if constexpr (MODE == WINDOW) {
+    int first = 0;   // WINDOW_PARTS: visited tiles ahead of the split's
+    if constexpr (WIN) {
         first_key = max(row0_wg + off + 1 - a.window, 0);
         near = max((min(a.sinks, kend_wg) + BC - 1) / BC, 0);
         gap = max(first_key / BC - near, 0);
-        ntiles -= gap;
+        ntiles = max(ntiles - gap, 0);
+    }
+    if constexpr (MODE == WINDOW_PARTS) {
+        split = wg - bid * (int)a.splits.d;
+        const int q = a.splits.div(ntiles), each = q + (q * (int)a.splits.d != ntiles);
+        first = min(split * each, ntiles);
+        ntiles = min(ntiles - first, each);
     }
     if constexpr (MODE == PARTS) {
         const int each = (ntiles + nsplit - 1) / nsplit;
@@ -338,12 +351,12 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
         koff[j] = r * row_bytes + 16 * (c ^ kswz(r));
         voff[j] = r * row_bytes + 16 * (c ^ vswz(r));
     }
-    // WINDOW, PARTS: bf16 V also goes to LDS directly, as it is, and becomes fp16 in its
+    // WINDOW, PARTS (and WINDOW_PARTS): bf16 V also goes to LDS directly, as it is, and becomes fp16 in its
     // place once it is there, so that no registers hold it during a step (window
     // 1024, 32/8 heads, D = 128, bf16: 4096 rows 90.1 -> 85.1 us, 8192 168.6 -> 160.8; with
     // five stages instead of three, and two waves per SIMD, 91.8 and 177.8; JOIN, 8 x
     // 256 rows behind 4096 + 512 keys, 157.8 against 154.2 through registers).
-    constexpr bool RAW = IN_BF16 && (MODE == WINDOW || MODE == PARTS), VREG = IN_BF16 && !RAW;
+    constexpr bool RAW = IN_BF16 && JUMPS, VREG = IN_BF16 && !RAW;
     typedef uint4_t vregs_t[VREG ? NP : 1];
     vregs_t vr;   // bf16: the next tile's V chunks, in flight during a step
     // Scalar state of the next tile to load: the address of its first key row
@@ -403,7 +416,7 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
     const unsigned lds0 = lds_address(smem);
     // the next tile (they are loaded in order) into stage `stage`; bf16 V into vr
     auto gload_to = [&](vregs_t &vr, int stage) __attribute__((always_inline)) {
-        if constexpr (MODE == WINDOW || MODE == PARTS) {
+        if constexpr (JUMPS) {
             if (gap > 0 && tload == near) go_to(near + gap);
         }
         if constexpr (SEGMENTS) {
@@ -420,7 +433,7 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
             // the address comes from the table (page numbers clamped into the
             // pool), within it the address advances by one tile per load
             if (poff == 0) {
-                if (pidx > 0 && pidx % 64 == 0 && MODE != WINDOW && MODE != PARTS) {
+                if (pidx > 0 && pidx % 64 == 0 && !JUMPS) {
                     tcur = tnx;
                     tnx = __builtin_amdgcn_raw_buffer_load_b32(trs, 4 * (pidx + 64 + l), 0, 0);
                 }
@@ -433,12 +446,12 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
         const int nrec = tload < full_tiles ? tile_bytes : last_bytes;
         // WINDOW: a tile with keys between the sinks and the window reads them as zeros
         int drop0 = 0, drop1 = 0;   // (rows of the tile)
-        if constexpr (MODE == WINDOW) {
+        if constexpr (WIN) {
             drop0 = max(a.sinks - tload * BC, 0);
             drop1 = first_key - tload * BC;
         }
         auto at = [&](int off, int j) {
-            if constexpr (MODE == WINDOW) {
+            if constexpr (WIN) {
                 const int r = (64 * (piece + (NT / 64) * j) + l) / CPR;
                 return r >= drop0 && r < drop1 ? (int)0x80000000 : off;
             } else {
@@ -476,7 +489,7 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
             const bool cross = poff == a.page_size;   // wave-uniform
             poff = cross ? 0 : poff;
             pidx += cross ? 1 : 0;
-            if constexpr (MODE == WINDOW || MODE == PARTS) {
+            if constexpr (JUMPS) {
                 if (cross && pidx % 64 == 0) {
                     tcur = tnx;
                     tnx = __builtin_amdgcn_raw_buffer_load_b32(trs, 4 * (pidx + 64 + l), 0, 0);
@@ -620,14 +633,14 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
                 kw += a.prefix - near * BC;
         }
         // WINDOW: the last key that the slot's last row does not see any more
-        const int passed = MODE == WINDOW ? row0 + WR - 1 + off - a.window : -1;
-        if (kw + 32 > (SEGMENTS ? min(kfree_w, end) : kfree_w) || (MODE == WINDOW && kw <= passed && kw + 32 > a.sinks)) {
+        const int passed = WIN ? row0 + WR - 1 + off - a.window : -1;
+        if (kw + 32 > (SEGMENTS ? min(kfree_w, end) : kfree_w) || (WIN && kw <= passed && kw + 32 > a.sinks)) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int key = kw + 8 * (r >> 2) + 4 * lh + (r & 3);
                 const bool vis = MODE == PARTS ? key < rlim
                                                 : key < end && (!CAUSAL || key <= qi + off) &&
-                                                      (MODE != WINDOW || key > qi + off - a.window || key < a.sinks);
+                                                      (!WIN || key > qi + off - a.window || key < a.sinks);
                 s[r] = vis ? s[r] : -INFINITY;
             }
         }
@@ -703,6 +716,9 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
     // the whole next step as well: step i waits for tile i + 1's, and writes its
     // bf16 V, after its own scores.  With two, at its end.
     constexpr int AHEAD = SM::AHEAD;
+    if constexpr (MODE == WINDOW_PARTS) {
+        if (first > 0 && ntiles > 0) go_to(first + (first >= near ? gap : 0));
+    }
     if (ntiles > 0) {
         vregs_t v0;
         gload_to(v0, 0);
@@ -720,9 +736,9 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
         // the next tile's loads are issued after the K operand reads (their
         // scalar set-up then overlaps the LDS latency, and at D = 128 their
         // registers are not live across the QK^T product)
-        const int t = i + ((MODE == WINDOW || MODE == PARTS) && i >= near ? gap : 0);   // the tile
+        const int t = first + i + (JUMPS && first + i >= near ? gap : 0);   // the tile
         bool some = true;   // some row of the wave sees some key of it (wave-uniform)
-        if constexpr (MODE == WINDOW) {
+        if constexpr (WIN) {
             const int kw = t * BC + 32 * kh;
             some = live && kw <= row0 + WR - 1 + off && (kw + 31 > row0 + off - a.window || kw < a.sinks);
         }
@@ -793,9 +809,10 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
         m_run = M;
     }
     const float l_tot = pair_sum(l_run);
-    if constexpr (MODE == PARTS) {
+    if constexpr (MODE == PARTS || MODE == WINDOW_PARTS) {
         if (qi >= Nq) return;
-        const size_t at = ((size_t)tok * a.Hq + h) * a.slots + split + (own ? (int)a.splits.d : 0);
+        const size_t token = MODE == PARTS ? (size_t)tok : (size_t)b * Nq + qi;
+        const size_t at = (token * a.Hq + h) * a.slots + split + (own ? (int)a.splits.d : 0);
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll

@@ -224,7 +224,7 @@ hipError_t launch_join(const PrefixProblem &pp, hipStream_t stream) {
 }
 
 template <typename TOUT>
-hipError_t launch_merge(const Problem &p, int slots, const float *ws, hipStream_t stream) {
+hipError_t launch_merge_t(const Problem &p, int slots, const float *ws, hipStream_t stream) {
     const long long rows = (long long)p.B * p.Nq * p.Hq;
     const size_t parts = (size_t)rows * slots;
     const float *m = ws + parts * p.D;
@@ -245,10 +245,15 @@ hipError_t launch_d(const PrefixProblem &pp, float *ws, hipStream_t stream) {
     if (n.prefix == 0)
         return p.D == 64 ? launch_join<TIN, TOUT, 64>(pp, stream) : launch_join<TIN, TOUT, 128>(pp, stream);
     const hipError_t e = p.D == 64 ? launch_parts<TIN, 64>(pp, n, ws, stream) : launch_parts<TIN, 128>(pp, n, ws, stream);
-    return e != hipSuccess ? e : launch_merge<TOUT>(p, n.prefix + n.own, ws, stream);
+    return e != hipSuccess ? e : launch_merge(p, n.prefix + n.own, ws, stream);
 }
 
 }  // namespace
+
+hipError_t launch_merge(const Problem &p, int slots, const float *ws, hipStream_t stream) {
+    if (p.out == FA_F32) return launch_merge_t<float>(p, slots, ws, stream);
+    return p.in == FA_F16 ? launch_merge_t<_Float16>(p, slots, ws, stream) : launch_merge_t<__bf16>(p, slots, ws, stream);
+}
 
 size_t prefix_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Np, int Nk, int D, bool most) {
     const Plan n = plan(B, Hq, Hkv, Nq, Np, Nk, D, most);

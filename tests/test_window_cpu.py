@@ -46,7 +46,12 @@ def test_workspace_sizes():
     assert 0 < need <= workspace_bytes(*a, "bf16")
     assert need == workspace_bytes(16, 32, 8, 1, 1028, 128, "bf16")
     assert window_workspace_bytes(*a, 1 << 40, "bf16", sinks=1 << 40) == workspace_bytes(*a, "bf16")
-    assert window_workspace_bytes(16, 32, 8, 2, 8192, 128, 1024, "bf16") == 0   # no split path
+    assert window_workspace_bytes(16, 32, 8, 512, 8192, 128, 1024, "bf16") == 0   # row blocks for all CUs: no parts
+    assert window_workspace_bytes(1, 32, 8, 8, 8192, 96, 1024, "bf16") == 0 and window_workspace_bytes(1, 2, 2, 9, 500, 64, 100, "f32") == 0
+    few = window_workspace_bytes(1, 32, 8, 8, 8192, 128, 4096, "bf16", sinks=4)
+    assert few > 0
+    for Nk in (8, 100, 4000, 4105, 8191):
+        assert window_workspace_bytes(1, 32, 8, 8, Nk, 128, 4096, "bf16", sinks=4) <= few
     assert window_workspace_bytes(*a, 0, "bf16") == 0 and window_workspace_bytes(*a, 5, "bf16", sinks=-1) == 0
     for Nk in (1, 700, 1027, 1029, 5000):
         assert window_workspace_bytes(16, 32, 8, 1, Nk, 128, 1024, "bf16", sinks=4) <= need

@@ -126,6 +126,13 @@ EDGES = [
     (2, 8, 8, 40, 10000, 64, "f16", 1000, 200, [10000, 9000], 64),        # tables of more than 64 pages, crossed in the window
     (1, 8, 8, 33, 9000, 128, "bf16", 4500, 4300, [8990], 64),             # and in the sinks
     (2, 4, 1, 2, 66, 64, "f16", 2, 1, [66, 1], 0),
+    # few row blocks and long windows: tiles split over workgroups; splits that begin in the sinks, in the window, with nothing
+    (2, 8, 2, 8, 9000, 128, "bf16", 4096, 4, [9000, 5000], 0),
+    (2, 8, 2, 8, 9000, 64, "f16", 4096, 700, [9000, 5], 64),
+    (1, 4, 4, 40, 9000, 128, "f16", 3000, 4000, [8200], 64),
+    (1, 16, 2, 33, 6000, 64, "bf16", 2500, 1, None, 0),
+    (3, 4, 1, 5, 5000, 128, "bf16", 5000, 0, [5000, 3, 0], 128),
+    (1, 3, 3, 200, 6000, 64, "bf16", 5900, 70, [5999], 0),
     # fp32 weights: fp32 inputs and other head sizes
     (2, 4, 2, 1, 333, 64, "f32", 50, 3, [333, 20], 0),
     (2, 4, 2, 100, 333, 40, "f32", 50, 3, [333, 60], 0),
@@ -198,6 +205,23 @@ def test_long_cache_rows_past_31_bits():
         a, la = fa.fwd_window(q, k, v, 100, out_dtype=torch.float32)
         b, lb = fa.fwd_window(q, k[:, -200:].contiguous(), v[:, -200:].contiguous(), 100, out_dtype=torch.float32)
         assert float((a - b).abs().max()) <= 6 * 2.0 ** -11 and float((la - lb).abs().max()) <= 2.0 ** -11
+
+
+def test_parts_workspace():
+    """Row blocks split over workgroups: with a workspace of the call's own, too small a one, and the library's."""
+    q, k, v = (t.cuda() for t in make_qkv(1, 32, 8, 9, 8000, 128, "bf16", seed=8))
+    need = fa.window_workspace_bytes(1, 32, 8, 9, 8000, 128, 4000, "bf16", sinks=4)
+    assert need > 0
+    ref, lse = fa.fwd_window(q, k, v, 4000, sinks=4)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    mine, mlse = fa.fwd_window(q, k, v, 4000, sinks=4, workspace=ws)
+    assert torch.equal(ref, mine) and torch.equal(lse, mlse)
+    with pytest.raises(fa.FaError) as e:
+        fa.fwd_window(q, k, v, 4000, sinks=4, workspace=ws[:1024])
+    assert e.value.status == 10
+    for Nk in (9, 40, 500, 3000, 4100):
+        fa.fwd_window(q, k[:, :Nk].contiguous(), v[:, :Nk].contiguous(), 4000, sinks=4, workspace=ws)
+    torch.cuda.synchronize()
 
 
 def test_workspaces():
