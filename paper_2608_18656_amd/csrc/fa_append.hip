@@ -13,8 +13,9 @@
 // row, those whose columns rotate together (both halves of the rotated columns,
 // or any two chunks where pairs are neighbours), so that it writes exactly what
 // it has read, and a rotation in place needs no barrier.
-// What bounds it: HBM for long prompts, the chain launch, lengths, table entry,
-// store for a step of single tokens.
+// What bounds it: HBM for long prompts (8192 tokens, 32/8 heads, D = 128, fp16: 34.8
+// us, 5.8 TB/s read and written; a large copy reaches 5.0), the chain launch,
+// lengths, table entry, store for a step of single tokens (64: 4.2 us).
 #include "fa_common.h"
 #include "fa_internal.h"
 
@@ -23,6 +24,12 @@ namespace {
 
 constexpr int NT = 256;           // threads per workgroup
 constexpr int MAX_PAIRS = 128;    // D <= 256
+// Bytes up to which the inputs are read through the caches.  A projection leaves its
+// result in the memory side's 256 MB, from where plain loads are quicker (5777
+// tokens, 16/2 heads, D = 128, 59 MB: 11.9 us, non-temporal 13.8); a long prompt's does
+// not stay there with what is written (8192 tokens, 32/8 heads, D = 128, 201 MB: 42.3
+// us, non-temporal 34.8; 131 MB 28.0 / 26.5).
+constexpr long long HELD = 128 << 20;
 
 struct AppendArgs {
     const void *q, *k, *v;
@@ -49,9 +56,15 @@ template <typename S> struct Chunk {
     typedef S vec __attribute__((ext_vector_type(16 / sizeof(S))));
 };
 
+// 16 bytes of an input; ONCE: past the caches.
+template <typename V, bool ONCE> __device__ __forceinline__ V load(const void *p) {
+    if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const V *>(p));
+    else return *reinterpret_cast<const V *>(p);
+}
+
 // VEC: chunks hold whole pairs (interleaved) or whole chunks pair (halves);
 // else single elements, any even number of rotated columns.
-template <typename S, bool VEC, int TB>
+template <typename S, bool VEC, int TB, bool ONCE>
 __global__ __launch_bounds__(NT) void append_kernel(AppendArgs a) {
     constexpr int E = Chunk<S>::E;
     typedef typename Chunk<S>::vec V;
@@ -118,7 +131,7 @@ __global__ __launch_bounds__(NT) void append_kernel(AppendArgs a) {
             if (rot > 0 && !a.interleaved) {
                 const int hc = rot / (2 * E);   // chunks of a half
                 if (u < hc) {
-                    V x = *reinterpret_cast<const V *>(src + E * u), y = *reinterpret_cast<const V *>(src + E * (u + hc));
+                    V x = load<V, ONCE>(src + E * u), y = load<V, ONCE>(src + E * (u + hc));
                     V xo, yo;
 #pragma unroll
                     for (int e = 0; e < E; ++e) {
@@ -131,26 +144,30 @@ __global__ __launch_bounds__(NT) void append_kernel(AppendArgs a) {
                     *reinterpret_cast<V *>(dst + E * (u + hc)) = yo;
                 } else {   // the columns past the rotated ones
                     const int rest = chunks - 2 * hc, n = (rest + 1) / 2, c0 = 2 * hc + (u - hc), c1 = c0 + n;
-                    const uint4_t x = ld16(src + E * c0);
-                    if (c1 < chunks) st16(dst + E * c1, ld16(src + E * c1));
-                    st16(dst + E * c0, x);
+                    const V x = load<V, ONCE>(src + E * c0);
+                    if (c1 < chunks) *reinterpret_cast<V *>(dst + E * c1) = load<V, ONCE>(src + E * c1);
+                    *reinterpret_cast<V *>(dst + E * c0) = x;
                 }
             } else {
+                const int c1 = u + (int)a.row_units.d;
+                const bool two = c1 < chunks;
+                V x[2];
+                x[0] = load<V, ONCE>(src + E * u);
+                if (two) x[1] = load<V, ONCE>(src + E * c1);
 #pragma unroll
                 for (int n = 0; n < 2; ++n) {
-                    const int c = u + n * (int)a.row_units.d;
-                    if (c >= chunks) break;
-                    V x = *reinterpret_cast<const V *>(src + E * c);
+                    const int c = n ? c1 : u;
+                    if (n && !two) break;
                     if (E * c < rot) {
 #pragma unroll
                         for (int e = 0; e < E; e += 2) {
                             const float2 w = tp[(E * c + e) / 2];
-                            const float f = (float)x[e], g = (float)x[e + 1];
-                            x[e] = from_f32<S>(f * w.x - g * w.y);
-                            x[e + 1] = from_f32<S>(f * w.y + g * w.x);
+                            const float f = (float)x[n][e], g = (float)x[n][e + 1];
+                            x[n][e] = from_f32<S>(f * w.x - g * w.y);
+                            x[n][e + 1] = from_f32<S>(f * w.y + g * w.x);
                         }
                     }
-                    *reinterpret_cast<V *>(dst + E * c) = x;
+                    *reinterpret_cast<V *>(dst + E * c) = x[n];
                 }
             }
         } else {   // unit u: a pair, or two of the columns past the rotated ones
@@ -176,10 +193,13 @@ hipError_t launch_t(AppendArgs &a, hipStream_t s) {
     a.units = Divisor((unsigned)rows * ru);
     constexpr int TB = 4;
     const unsigned blocks = ((unsigned)a.tokens + TB - 1) / TB;
+    const long long bytes = 2LL * a.tokens * rows * a.D * sizeof(S);   // read and written
     if (a.tokens <= 1024)   // a workgroup each
-        hipLaunchKernelGGL((append_kernel<S, VEC, 1>), dim3((unsigned)a.tokens), dim3(NT), 0, s, a);
+        hipLaunchKernelGGL((append_kernel<S, VEC, 1, false>), dim3((unsigned)a.tokens), dim3(NT), 0, s, a);
+    else if (bytes <= HELD)
+        hipLaunchKernelGGL((append_kernel<S, VEC, TB, false>), dim3(blocks), dim3(NT), 0, s, a);
     else
-        hipLaunchKernelGGL((append_kernel<S, VEC, TB>), dim3(blocks), dim3(NT), 0, s, a);
+        hipLaunchKernelGGL((append_kernel<S, VEC, TB, true>), dim3(blocks), dim3(NT), 0, s, a);
     return hipGetLastError();
 }
 
