@@ -60,3 +60,10 @@ def test_workspace_sizes():
         a = dict(B=2, Hq=4, Hkv=2, Nq=1, Np=100, Nk=100, D=64, in_dtype="f16")
         a.update(over)
         assert prefix_workspace_bytes(**a) == 0
+
+
+def test_key_rows_past_32_bit_offsets_are_refused():
+    far = {n: (i + 1) << 44 for i, n in enumerate(("q", "kp", "vp", "k", "v", "o", "lse", "lens", "table", "ws"))}
+    for D, last in ((128, 270600), (64, 266304)):
+        for paged in (False, True):
+            assert prefix(paged, Hq=last + 1, Hkv=last + 1, B=1, D=D, Np=8000, wb=1 << 50, **far) == 2

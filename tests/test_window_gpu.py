@@ -239,3 +239,25 @@ def test_workspaces():
     for Nk in (1, 31, 500, 2047, 2053, 4000):
         fa.fwd_window(q, k[:, :Nk].contiguous(), v[:, :Nk].contiguous(), 2048, sinks=4, workspace=ws)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("D,H,Nq", [(128, 270601, 1), (128, 270601, 4), (64, 270601, 3)])
+def test_key_rows_past_32_bit_offsets(D, H, Nq):
+    """Tiles of more than 2 GiB, contiguous and in pages of which the middle one is not seen."""
+    gen = torch.Generator("cuda").manual_seed(6)
+    Nk, W, S = 160, 20, 2
+    k, v = (torch.randn(1, 192, H, D, generator=gen, device="cuda", dtype=torch.float16) for _ in range(2))
+    q = torch.randn(1, Nq, H, D, generator=gen, device="cuda", dtype=torch.float16)
+    n = torch.tensor([Nk], dtype=torch.int32, device="cuda")
+    o, lse = fa.fwd_window(q, k, v, W, sinks=S, seqlens_k=n, out_dtype=torch.float32)
+    table = torch.tensor([[0, 1 << 20, 2]], dtype=torch.int32, device="cuda")
+    op, lp = fa.fwd_window_paged(q, k.view(3, 64, H, D), v.view(3, 64, H, D), table, n, W, sinks=S, out_dtype=torch.float32)
+    assert torch.equal(o, op) and torch.equal(lse, lp)
+    for h0 in range(0, H, 16384):
+        h = slice(h0, h0 + 16384)
+        for i in range(Nq):
+            p = Nk - Nq + i
+            see = list(range(S)) + list(range(p - W + 1, p + 1))
+            w = torch.softmax((q[0, i, h].double() * k[0, see, h].double()).sum(-1) * default_scale(D), 0)
+            ref = (w[:, :, None] * v[0, see, h].double()).sum(0)
+            assert (o[0, i, h].double() - ref).abs().max().item() <= 2e-3, (h0, i)
