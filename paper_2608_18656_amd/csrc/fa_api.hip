@@ -568,10 +568,12 @@ fa_status_t fa_fwd_window_paged(const void *q, const void *k_pages, const void *
 
 size_t fa_window_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Nk, int D, int window, int sinks,
                                  fa_dtype_t in_dtype) {
-    if (window < 1 || sinks < 0 || B < 1 || Hq < 1 || Hkv < 1 || Nk < 1 || Hq % Hkv != 0) return 0;
+    if (window < 1 || sinks < 0 || B < 1 || Hq < 1 || Hkv < 1 || Nq < 1 || Nk < 1 || Hq % Hkv != 0 ||
+        (long long)B * Nq > 0x7fffffffLL)
+        return 0;
     if (fa::decode_supported(Nq, Hkv, D, in_dtype))
         return fa::decode_workspace_bytes(B, Hq, D, decode_splits(B, Hq, Hkv, Nk, D, Window{window, sinks}, true));
-    return Nq >= 1 && fa::prefill_supported(Hkv, D, in_dtype)
+    return fa::prefill_supported(Hkv, D, in_dtype)
                ? fa::window_workspace_bytes(B, Hq, Hkv, Nq, Nk, D, window, sinks, true) : 0;
 }
 
