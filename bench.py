@@ -38,6 +38,7 @@ PEAK_MFMA_TFLOPS = {"bf16": 2500.0, "f16": 2500.0, "f32": 157.3}   # dense, MI35
 PEAK_HBM_GBS = 8000.0
 METRIC = "prefill attention TFLOP/s (% MFMA peak); decode KV GB/s (% HBM peak)"
 PREFILL_SOURCES = ["paper_2608_18656_amd/csrc/fa_prefill.hip",
+                   "paper_2608_18656_amd/csrc/fa_prefill_kernel.h",
                    "paper_2608_18656_amd/csrc/fa_common.h"]
 DECODE_SOURCES = ["paper_2608_18656_amd/csrc/fa_decode.hip",
                   "paper_2608_18656_amd/csrc/fa_common.h"]

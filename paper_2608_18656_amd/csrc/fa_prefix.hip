@@ -24,30 +24,28 @@ constexpr int CUS = 256;                 // compute units of the card
 constexpr int MIN_TILES = 4;             // least tiles in a split of the prefix
 constexpr int ROWS = WR * NSLOT;         // rows of a workgroup against the prefix
 
-// One wave per row: partial results of `slots` parts merged, D / 64 columns a lane.
-template <typename TOUT, int D>
+// Partial results of `slots` parts merged, D / 64 columns a lane.  A row's parts are
+// taken by one wave, eight loads together, or dealt out to the four of the
+// workgroup, whose results are merged through LDS (WPR; a chain of loads the
+// fewer for the long lists that few rows have: 2 x 32/4 heads, 64 parts, 16.5 -> 13.7
+// us a call).
+constexpr int LONG_LIST = 16;   // parts from which four waves share a row
+
+template <typename TOUT, int D, int WPR>
 __global__ __launch_bounds__(256) void merge_kernel(const float *__restrict__ opart, const float *__restrict__ mpart,
                                                     const float *__restrict__ lpart, void *o, float *lse, int slots,
                                                     int rows, int Hq, int Nq) {
     constexpr int N = D / 64;
     typedef float vec __attribute__((ext_vector_type(N)));
     typedef TOUT out __attribute__((ext_vector_type(N)));
-    const int l = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int l = threadIdx.x & 63, w = threadIdx.x >> 6, row = WPR == 1 ? blockIdx.x * 4 + w : blockIdx.x;
     if (row >= rows) return;
+    const int each = (slots + WPR - 1) / WPR, first = WPR == 1 ? 0 : min(w * each, slots), end = min(first + each, slots);
     const float *mp = mpart + (size_t)row * slots, *lp = lpart + (size_t)row * slots;
     const float *op = opart + (size_t)row * slots * D + N * l;
     float M = -INFINITY, L = 0.f;
     vec acc = vec{};
-    for (int s0 = 0; s0 < slots; s0 += 8) {   // eight parts' loads together
-        float m[8], w[8];
-        vec x[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int s = min(s0 + j, slots - 1);
-            m[j] = s0 + j < slots ? mp[s] : -INFINITY;
-            w[j] = lp[s];
-            x[j] = *reinterpret_cast<const vec *>(op + (size_t)s * D);
-        }
+    auto add = [&](const float (&m)[8], const float (&n)[8], const vec (&x)[8]) {
         float Mc = M;
 #pragma unroll
         for (int j = 0; j < 8; ++j) Mc = __builtin_fmaxf(Mc, m[j]);
@@ -57,11 +55,46 @@ __global__ __launch_bounds__(256) void merge_kernel(const float *__restrict__ op
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const float f = m[j] == -INFINITY ? 0.f : exp2_fast(m[j] - Mc);
-            L = __builtin_fmaf(f, w[j], L);
+            L = __builtin_fmaf(f, n[j], L);
 #pragma unroll
-            for (int n = 0; n < N; ++n) acc[n] = __builtin_fmaf(f, x[j][n], acc[n]);
+            for (int c = 0; c < N; ++c) acc[c] = __builtin_fmaf(f, x[j][c], acc[c]);
         }
         M = Mc;
+    };
+    for (int s0 = first; s0 < end; s0 += 8) {
+        float m[8], n[8];
+        vec x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int s = min(s0 + j, end - 1);
+            m[j] = s0 + j < end ? mp[s] : -INFINITY;
+            n[j] = lp[s];
+            x[j] = *reinterpret_cast<const vec *>(op + (size_t)s * D);
+        }
+        add(m, n, x);
+    }
+    if constexpr (WPR > 1) {
+        __shared__ float part[WPR][D + 2];
+        *reinterpret_cast<vec *>(&part[w][N * l]) = acc;
+        if (l == 0) {
+            part[w][D] = M;
+            part[w][D + 1] = L;
+        }
+        __syncthreads();
+        if (w > 0) return;
+        float m[8], n[8];
+        vec x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int i = j < WPR ? j : 0;
+            m[j] = j < WPR ? part[i][D] : -INFINITY;
+            n[j] = part[i][D + 1];
+            x[j] = *reinterpret_cast<const vec *>(&part[i][N * l]);
+        }
+        M = -INFINITY;
+        L = 0.f;
+        acc = vec{};
+        add(m, n, x);
     }
     // a row that sees no key gives 0 and -inf
     const float inv = L > 0.f ? 1.f / L : 0.f;
@@ -223,19 +256,23 @@ hipError_t launch_join(const PrefixProblem &pp, hipStream_t stream) {
     return hipGetLastError();
 }
 
-template <typename TOUT>
+template <typename TOUT, int D>
 hipError_t launch_merge_t(const Problem &p, int slots, const float *ws, hipStream_t stream) {
     const long long rows = (long long)p.B * p.Nq * p.Hq;
     const size_t parts = (size_t)rows * slots;
-    const float *m = ws + parts * p.D;
-    const dim3 grid((unsigned)((rows + 3) / 4));
-    if (p.D == 64)
-        hipLaunchKernelGGL((merge_kernel<TOUT, 64>), grid, dim3(256), 0, stream, ws, m, m + parts, p.o, p.lse, slots,
-                           (int)rows, p.Hq, p.Nq);
+    const float *m = ws + parts * D;
+    if (slots > LONG_LIST)
+        hipLaunchKernelGGL((merge_kernel<TOUT, D, 4>), dim3((unsigned)rows), dim3(256), 0, stream, ws, m, m + parts, p.o,
+                           p.lse, slots, (int)rows, p.Hq, p.Nq);
     else
-        hipLaunchKernelGGL((merge_kernel<TOUT, 128>), grid, dim3(256), 0, stream, ws, m, m + parts, p.o, p.lse, slots,
-                           (int)rows, p.Hq, p.Nq);
+        hipLaunchKernelGGL((merge_kernel<TOUT, D, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, ws, m,
+                           m + parts, p.o, p.lse, slots, (int)rows, p.Hq, p.Nq);
     return hipGetLastError();
+}
+
+template <typename TOUT>
+hipError_t launch_merge_d(const Problem &p, int slots, const float *ws, hipStream_t stream) {
+    return p.D == 64 ? launch_merge_t<TOUT, 64>(p, slots, ws, stream) : launch_merge_t<TOUT, 128>(p, slots, ws, stream);
 }
 
 template <typename TIN, typename TOUT>
@@ -251,8 +288,8 @@ hipError_t launch_d(const PrefixProblem &pp, float *ws, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_merge(const Problem &p, int slots, const float *ws, hipStream_t stream) {
-    if (p.out == FA_F32) return launch_merge_t<float>(p, slots, ws, stream);
-    return p.in == FA_F16 ? launch_merge_t<_Float16>(p, slots, ws, stream) : launch_merge_t<__bf16>(p, slots, ws, stream);
+    if (p.out == FA_F32) return launch_merge_d<float>(p, slots, ws, stream);
+    return p.in == FA_F16 ? launch_merge_d<_Float16>(p, slots, ws, stream) : launch_merge_d<__bf16>(p, slots, ws, stream);
 }
 
 size_t prefix_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Np, int Nk, int D, bool most) {
