@@ -267,8 +267,8 @@ fa_status_t fa_set_workspace(void *dev_ptr, size_t bytes);
  * different streams) must pass disjoint workspaces.  Errors (before any HIP
  * call), on the split-KV path: FA_ERR_NULL for a NULL workspace,
  * FA_ERR_ALIGN for a misaligned one, FA_ERR_WORKSPACE when workspace_bytes is
- * too small, FA_ERR_ALIAS when it overlaps q, k, v, o or lse; otherwise as
- * fa_fwd_splitkv. */
+ * too small, FA_ERR_ALIAS when it overlaps q, k, v, o, lse, the lengths or the
+ * table; otherwise as fa_fwd_splitkv. */
 fa_status_t fa_fwd_ws(const void *q, const void *k, const void *v, void *o, float *lse, int B,
                       int Hq, int Hkv, int Nq, int Nk, int D, int causal, float scale, void *stream,
                       fa_dtype_t in_dtype, fa_dtype_t out_dtype, int num_splits, void *workspace,
@@ -381,6 +381,7 @@ fa_status_t fa_q8_0_gemv(const void *w, const void *x, void *y, int M, int K, fa
  *              call; ignored with one axis) */
 #define FA_MAX_AXES 4
 #define FA_MAX_ROTARY_PAIRS 128
+#define FA_MAX_APPEND_TOKENS (1 << 25)
 typedef struct {
     const float *inv_freq;
     const int *positions;
@@ -409,7 +410,7 @@ typedef struct {
  * Errors (before any HIP call): FA_ERR_NULL for a NULL k, v, cache, length
  * array or inv_freq, or one of q and q_out alone; FA_ERR_DIM for a size < 1,
  * a stride below the row or sizes too large ((Hq + 2 Hkv) * D above 2^28, B *
- * Nq above 2^31 - 1); FA_ERR_DTYPE; FA_ERR_GQA_RATIO (with q); FA_ERR_HEAD_DIM
+ * Nq above FA_MAX_APPEND_TOKENS); FA_ERR_DTYPE; FA_ERR_GQA_RATIO (with q); FA_ERR_HEAD_DIM
  * for D not a multiple of 8 or above 256; FA_ERR_ROTARY for a rot_dim, axes or
  * pair_axis out of range or several axes without positions; FA_ERR_ALIGN for a
  * tensor pointer or token stride not a multiple of 16 bytes, an int32 or float
@@ -489,8 +490,8 @@ size_t fa_window_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Nk, int D, 
  * that sees none gives 0 and -inf).  fp16 / bf16 with D in {64, 128}.
  * workspace, workspace_bytes: device scratch of this call
  * (fa_prefix_workspace_bytes), 16-byte aligned, or NULL and 0: the library's or
- * the one that is set (see the top); calls that need none ignore it.  Graphs that may run at the same time need
- * workspaces of their own.
+ * the one that is set (see the top); calls that need none ignore it.  Graphs
+ * that may run at the same time need workspaces of their own.
  * Errors: FA_ERR_NULL for a NULL tensor (or workspace with a size), FA_ERR_DIM
  * for a size < 1, Np + Nk above FA_MAX_PREFIX_KEYS, B * Nq * Hq above 2^31 - 1 or
  * key rows above 33 MiB, FA_ERR_DTYPE for fp32 inputs, FA_ERR_HEAD_DIM for another
@@ -506,10 +507,10 @@ fa_status_t fa_fwd_prefix(const void *q, const void *k_prefix, const void *v_pre
 /* fa_fwd_prefix against the paged cache of fa_fwd_kvcache_paged, the arguments
  * and the result of that call (lengths count the prefix; a sequence may be
  * shorter than it): the first prefix_len keys of all sequences are in the same
- * pages, and every row of the table names them.  prefix_len: a positive multiple of page_size, at most
- * page_size * max_pages.  Workspace: fa_prefix_workspace_bytes with Np =
- * prefix_len, Nk = page_size * max_pages - prefix_len.  Errors: FA_ERR_DIM for
- * another prefix_len; otherwise those of fa_fwd_prefix and fa_fwd_kvcache_paged. */
+ * pages, and every row of the table names them.  prefix_len: a positive multiple
+ * of page_size, at most page_size * max_pages.  Workspace:
+ * fa_prefix_workspace_bytes with Np = prefix_len, Nk = page_size * max_pages -
+ * prefix_len.  Errors: FA_ERR_DIM for another prefix_len; otherwise those of fa_fwd_prefix and fa_fwd_kvcache_paged. */
 fa_status_t fa_fwd_prefix_paged(const void *q, const void *k_pages, const void *v_pages, void *o,
                                 float *lse, const int *seqlens_k, const int *block_table, int B,
                                 int Hq, int Hkv, int Nq, int D, int page_size, int max_pages,

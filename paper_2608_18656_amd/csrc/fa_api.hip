@@ -4,6 +4,7 @@
 
 #include <cmath>
 #include <cstdint>
+#include <exception>
 #include <mutex>
 #include <vector>
 
@@ -71,6 +72,12 @@ fa_status_t get_workspace(size_t need, size_t room, hipStream_t stream, void **o
     if (cs != hipStreamCaptureStatusNone) return FA_ERR_WORKSPACE;
     const size_t sz = room < ((size_t)1 << 20) ? ((size_t)1 << 20) : room;
     void *ptr = nullptr;
+    try {   // room in the lists first: no exception may leave a C entry
+        g_retired.reserve(g_retired.size() + 1);
+        g_owned.reserve(g_owned.size() + 1);
+    } catch (const std::exception &) {
+        return FA_ERR_WORKSPACE;
+    }
     if (hipMalloc(&ptr, sz) != hipSuccess) {
         (void)hipGetLastError();
         return FA_ERR_WORKSPACE;
@@ -195,7 +202,9 @@ fa_status_t run(const void *q, const void *k, const void *v, void *o, float *lse
             const size_t kb = (size_t)(kv_rows < 0 ? (long long)B * Nk : kv_rows) * Hkv * D * esize(in);
             const size_t ob = (size_t)B * Nq * Hq * D * esize(out), lb = (size_t)B * Hq * Nq * sizeof(float);
             if (overlaps(ws, need, q, qb) || overlaps(ws, need, k, kb) || overlaps(ws, need, v, kb) ||
-                overlaps(ws, need, o, ob) || (lse && overlaps(ws, need, lse, lb)))
+                overlaps(ws, need, o, ob) || (lse && overlaps(ws, need, lse, lb)) ||
+                (seqlens && overlaps(ws, need, seqlens, (size_t)B * sizeof(int))) ||
+                (pg.block_table && overlaps(ws, need, pg.block_table, (size_t)B * pg.max_pages * sizeof(int))))
                 return FA_ERR_ALIAS;
         }
     }

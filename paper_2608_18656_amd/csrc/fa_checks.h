@@ -92,7 +92,7 @@ inline fa_status_t validate_append(const void *k, const void *v, const void *k_c
     if (q && Hq % Hkv != 0) return FA_ERR_GQA_RATIO;
     if (D % 8 != 0 || D > 256) return FA_ERR_HEAD_DIM;
     const long long heads = (q ? Hq : 0) + 2LL * Hkv, tokens = (long long)B * N;
-    if (heads * D > (1LL << 28) || tokens > 0x7fffffffLL) return FA_ERR_DIM;
+    if (heads * D > (1LL << 28) || tokens > FA_MAX_APPEND_TOKENS) return FA_ERR_DIM;
     if ((q && qs < (long long)Hq * D) || ks < (long long)Hkv * D || vs < (long long)Hkv * D) return FA_ERR_DIM;
     long long nq = 0, nk, nv, nc;
     if ((q && !mul_ok(tokens, qs, &nq)) || !mul_ok(tokens, ks, &nk) || !mul_ok(tokens, vs, &nv) ||

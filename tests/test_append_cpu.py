@@ -80,3 +80,10 @@ def test_refusals_paged(over, code):
 def test_refusals_of_the_rotation(over, code):
     assert append(rot=rotary(**over)) == code
     assert append(rot=rotary(**over), paged=True) == code
+
+
+def test_more_tokens_than_a_grid_takes_are_refused():
+    far = {n: (i + 1) << 44 for i, n in enumerate(("k", "v", "kc", "vc", "q", "qo", "lens", "table"))}
+    for B, N in (((1 << 25) + 1, 1), (1 << 13, (1 << 12) + 1), (1, 1 << 30)):
+        for paged in (False, True):
+            assert append(paged=paged, B=B, N=N, mp=1, **far) == 2

@@ -55,3 +55,7 @@ def test_workspace_sizes():
     assert window_workspace_bytes(*a, 0, "bf16") == 0 and window_workspace_bytes(*a, 5, "bf16", sinks=-1) == 0
     for Nk in (1, 700, 1027, 1029, 5000):
         assert window_workspace_bytes(16, 32, 8, 1, Nk, 128, 1024, "bf16", sinks=4) <= need
+
+
+def test_workspace_apart_from_lengths_and_table():
+    assert window(False, ws=6 * M) == 8 and window(True, ws=6 * M) == 8 and window(True, ws=7 * M) == 8
