@@ -54,6 +54,10 @@ struct AppendProblem {
     int page_size, max_pages, num_pages;
 };
 
+// Whether a grid of `blocks` workgroups of `threads` can be launched: its threads are
+// counted in 32 bits.
+inline bool grid_fits(long long blocks, int threads) { return blocks <= 0xffffffffLL / threads; }
+
 // Each launcher enqueues its kernels on `stream` and returns the first HIP
 // error (hipSuccess when the launch was accepted).
 hipError_t launch_prefill(const Problem &p, hipStream_t stream);

@@ -218,7 +218,9 @@ hipError_t launch_parts(const PrefixProblem &pp, const Plan &n, float *ws, hipSt
     a.first_page = p.block_table ? pp.Np / p.page_size : 0;
     const long long shared = (rows + ROWS - 1) / ROWS * p.Hkv * n.prefix;
     const long long nblocks = shared + ((long long)p.Nq * G + ROWS - 1) / ROWS * p.B * p.Hkv * n.own;
-    if (nblocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    // (also the merge's, whose launch comes second: a wave or a workgroup a row)
+    if (!grid_fits(nblocks, SM::NT) || !grid_fits(rows * p.Hkv, a.slots > LONG_LIST ? 256 : 64))
+        return hipErrorInvalidConfiguration;
     a.prefix_blocks = (int)shared;
     if (p.block_table)
         hipLaunchKernelGGL((prefill_kernel<TIN, float, D, NSLOT, false, true, PARTS>), dim3((unsigned)nblocks),
@@ -241,7 +243,7 @@ hipError_t launch_join(const PrefixProblem &pp, hipStream_t stream) {
     const int RB = NSLOT / a.HW;
     a.nmb = a.first = (p.Nq + WR * RB - 1) / (WR * RB);
     const long long nblocks = (long long)a.nmb * p.B * p.Hkv * (G / a.HW);
-    if (nblocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    if (!grid_fits(nblocks, SM::NT)) return hipErrorInvalidConfiguration;
     a.nhg = Divisor(G / a.HW);
     a.per_mb = Divisor((unsigned)p.B * p.Hkv * (G / a.HW));
     const dim3 grid((unsigned)nblocks), block(SM::NT);

@@ -36,7 +36,7 @@ int splits_of(int B, int Hq, int Hkv, int Nq, int Nk, int D, int window, int sin
 
 template <typename TIN, typename TOUT, int D, int MODE>
 hipError_t launch_mode(const PrefillArgs &a, bool paged, long long blocks, hipStream_t stream) {
-    if (blocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    if (!grid_fits(blocks, Cfg<D>::NT)) return hipErrorInvalidConfiguration;
     const dim3 grid((unsigned)blocks), block(Cfg<D>::NT);
     if (paged)
         hipLaunchKernelGGL((prefill_kernel<TIN, TOUT, D, NSLOT, true, true, MODE>), grid, block, 0, stream, a);
