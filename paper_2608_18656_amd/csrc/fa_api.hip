@@ -72,9 +72,11 @@ fa_status_t get_workspace(size_t need, size_t room, hipStream_t stream, void **o
     if (cs != hipStreamCaptureStatusNone) return FA_ERR_WORKSPACE;
     const size_t sz = room < ((size_t)1 << 20) ? ((size_t)1 << 20) : room;
     void *ptr = nullptr;
-    try {   // room in the lists first: no exception may leave a C entry
-        g_retired.reserve(g_retired.size() + 1);
-        g_owned.reserve(g_owned.size() + 1);
+    // room in the list that grows first: no exception may leave a C entry.  (Not in
+    // g_owned with cur, which points into it.)
+    try {
+        if (cur) g_retired.reserve(g_retired.size() + 1);
+        else g_owned.reserve(g_owned.size() + 1);
     } catch (const std::exception &) {
         return FA_ERR_WORKSPACE;
     }

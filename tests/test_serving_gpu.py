@@ -273,3 +273,34 @@ def test_bitwise_determinism():
     for _ in range(5):
         b = fa.fwd_prefix(q, kp, kp, k, k)
         assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_outgrown_workspace_is_the_streams_own_from_then_on():
+    """A stream's library-owned workspace, outgrown by larger calls on several streams, is the larger one
+    from then on: the same calls are captured (where nothing may be allocated) and replay the eager results."""
+    gen = torch.Generator("cuda").manual_seed(11)
+    kp, vp = (torch.randn(1000, 4, 128, generator=gen, device="cuda", dtype=BF) for _ in range(2))
+    calls = []
+    for n in (1, 40):
+        q, k, v = (torch.randn(n, m, h, 128, generator=gen, device="cuda", dtype=BF) for m, h in ((1, 16), (90, 4), (90, 4)))
+        calls.append((q, kp, vp, k, v))
+    assert fa.prefix_workspace_bytes(1, 16, 4, 1, 1000, 90, 128, "bf16") < 1 << 20
+    assert fa.prefix_workspace_bytes(40, 16, 4, 1, 1000, 90, 128, "bf16") > 1 << 20
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    eager = []
+    for small_or_large in calls:
+        for st in streams:
+            with torch.cuda.stream(st):
+                eager.append(fa.fwd_prefix(*small_or_large))
+    torch.cuda.synchronize()
+    for st, (o, lse) in zip(streams, eager[3:]):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=st):
+            og, lg = fa.fwd_prefix(*calls[1])
+        for _ in range(3):
+            og.zero_()
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(og, o) and torch.equal(lg, lse)
