@@ -214,7 +214,7 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
     int mb = q_ < a.first ? a.nmb - 1 - q_ : q_ - a.first;
     int rest = bid - q_ * a.per_mb.d;
     int b = -1, len = a.Nk;
-    if (MODE == ALL && a.ranked > 0) {
+    if ((MODE == ALL || MODE == WINDOW) && a.ranked > 0) {
         const Lengths lens(a.seqlens, a.B, l);
         if (lens.uneven()) {
             const int u = a.per_seq.div(bid);
@@ -244,7 +244,7 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
         part_row0 = b0 * a.Nq * a.G;
         part_rows = own ? part_row0 + a.Nq * a.G : a.rows;
     }
-    if (MODE != ALL || a.ranked == 0) {
+    if ((MODE != ALL && MODE != WINDOW) || a.ranked == 0) {
         b = b0;
         if (MODE != PARTS && a.seqlens) len = a.seqlens[b];
     }
@@ -273,17 +273,21 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
     int kfree_w = CAUSAL ? min(Nk, row0 + off + 1) : Nk;
     int ntiles = (kend_wg + BC - 1) / BC;
     // The tiles visited: the first `near` ones and those from near + gap on.
-    // WINDOW: the sinks' and, from the first row's window on, the others; the
-    // keys between, from the last sink to first_key, count as not there, so that
-    // what they hold has no part in the result.
+    // WINDOW: the sinks' and, from the first row's window on (first_key), the others.
+    // The keys between count as not there, so that what they hold has no part in the
+    // result: the view of the last sink's tile ends, and that of the window's first
+    // tile begins, at the key itself.  That can be one tile, visited twice (gap -1).
+    // Sinks that reach the window are no part of their own.
     // JOIN: the prefix's tiles are the first `near`, the own ones follow.
-    int near = 0, gap = 0, first_key = 0;
+    int near = 0, gap = 0, first_key = 0, sinks = 0;   // sinks: in a part of their own
     int rlim = 0;   // PARTS: keys of the part that the lane's row sees
     int first = 0;   // WINDOW_PARTS: visited tiles ahead of the split's
     if constexpr (WIN) {
         first_key = max(row0_wg + off + 1 - a.window, 0);
-        near = max((min(a.sinks, kend_wg) + BC - 1) / BC, 0);
-        gap = max(first_key / BC - near, 0);
+        first_key = first_key > a.sinks ? first_key : 0;
+        sinks = first_key > 0 ? a.sinks : 0;
+        near = (sinks + BC - 1) / BC;
+        gap = first_key / BC - near;
         ntiles = max(ntiles - gap, 0);
     }
     if constexpr (MODE == WINDOW_PARTS) {
@@ -372,9 +376,9 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
     const S *vtile = vbase + (PAGED ? 0 : prefix_first ? (size_t)g * D : head0);
     const int tile_bytes = (BC - 1) * row_bytes + D * (int)sizeof(S);
     auto bytes_of = [&](int rows) { return rows > 0 ? (rows - 1) * row_bytes + D * (int)sizeof(S) : 0; };
-    int full_tiles = SEGMENTS ? a.prefix / BC : Nk / BC;
+    int full_tiles = SEGMENTS ? a.prefix / BC : Nk / BC - gap;   // (of those visited)
     int last_bytes = bytes_of(SEGMENTS ? a.prefix % BC : Nk % BC);
-    int tload = 0;
+    int tload = JUMPS ? first : 0;   // tiles visited ahead of it
     // paged K/V: the pool of pages, at head g.  Tiles are loaded in order
     // and a page holds a whole number of tiles, so the page index and the
     // offset inside the page advance without a division.  The wave holds 64
@@ -396,29 +400,33 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
         tcur = __builtin_amdgcn_raw_buffer_load_b32(trs, 4 * l, 0, 0);
         tnx = __builtin_amdgcn_raw_buffer_load_b32(trs, 4 * (64 + l), 0, 0);
     }
-    // to tile t, past the ones that are not visited
-    auto go_to = [&](int t) {
-        ktile += (size_t)(t - tload) * BC * row_elems;
-        vtile += (size_t)(t - tload) * BC * row_elems;
-        tload = t;
+    // past the tiles that are not visited: to tile t, from tile 0; paged: to key `key` of
+    // page `page`
+    auto go_to_page = [&](int page, int key) __attribute__((always_inline)) {
+        pidx = page;
+        poff = key;
+        const int at = 4 * ((pidx & ~63) + l);
+        tcur = __builtin_amdgcn_raw_buffer_load_b32(trs, at, 0, 0);
+        tnx = __builtin_amdgcn_raw_buffer_load_b32(trs, at + 256, 0, 0);
+        const int p = min(max(__builtin_amdgcn_readlane(tcur, pidx % 64), 0), a.num_pages - 1);
+        const size_t e = (size_t)g * D + (size_t)p * page_elems + (size_t)poff * row_elems;
+        ktile = kbase + e;
+        vtile = vbase + e;
+    };
+    const int far_page = WIN && PAGED ? (int)a.page_div.div((unsigned)(near + gap) * BC) : 0;   // of the window's first tile
+    const int far_key = WIN && PAGED ? (near + gap) * BC - far_page * a.page_size : 0;
+    auto go_to = [&](int t) __attribute__((always_inline)) {
         if constexpr (PAGED) {
-            pidx = a.page_div.div((unsigned)t * BC);
-            poff = t * BC - pidx * a.page_size;
-            const int at = 4 * ((pidx & ~63) + l);
-            tcur = __builtin_amdgcn_raw_buffer_load_b32(trs, at, 0, 0);
-            tnx = __builtin_amdgcn_raw_buffer_load_b32(trs, at + 256, 0, 0);
-            const int page = min(max(__builtin_amdgcn_readlane(tcur, pidx % 64), 0), a.num_pages - 1);
-            const size_t e = (size_t)g * D + (size_t)page * page_elems + (size_t)poff * row_elems;
-            ktile = kbase + e;
-            vtile = vbase + e;
+            const int page = a.page_div.div((unsigned)t * BC);
+            go_to_page(page, t * BC - page * a.page_size);
+        } else {
+            ktile += (size_t)t * BC * row_elems;
+            vtile += (size_t)t * BC * row_elems;
         }
     };
     const unsigned lds0 = lds_address(smem);
     // the next tile (they are loaded in order) into stage `stage`; bf16 V into vr
     auto gload_to = [&](vregs_t &vr, int stage) __attribute__((always_inline)) {
-        if constexpr (JUMPS) {
-            if (gap > 0 && tload == near) go_to(near + gap);
-        }
         if constexpr (SEGMENTS) {
             if (tload == near) {   // on to the sequence's own keys
                 ktile = reinterpret_cast<const S *>(a.k) + head0;
@@ -444,44 +452,47 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
             }
         }
         const int nrec = tload < full_tiles ? tile_bytes : last_bytes;
-        // WINDOW: a tile with keys between the sinks and the window reads them as zeros
-        int drop0 = 0, drop1 = 0;   // (rows of the tile)
-        if constexpr (WIN) {
-            drop0 = max(a.sinks - tload * BC, 0);
-            drop1 = first_key - tload * BC;
-        }
-        auto at = [&](int off, int j) {
-            if constexpr (WIN) {
-                const int r = (64 * (piece + (NT / 64) * j) + l) / CPR;
-                return r >= drop0 && r < drop1 ? (int)0x80000000 : off;
-            } else {
-                return off;
-            }
-        };
-        ++tload;
+        const int at = tload++;
         const unsigned dst = lds0 + stage * (2 * SM::STAGE) + 1024 * piece;
-        auto issue = [&](auto once) {   // once: nobody else reads these keys
+        // once: nobody else reads these keys; the view without `ahead` bytes at its start
+        // (offsets there wrap and read as zeros)
+        auto issue = [&](auto once, int nrec, auto ahead) __attribute__((always_inline)) {
             constexpr bool ONCE = decltype(once)::value;
             if (dok) {
 #pragma unroll
                 for (int j = 0; j < NP; ++j)
-                    load_lds16<ONCE>(ktile, nrec, dst + 1024 * (NT / 64) * j, at(koff[j], j));
+                    load_lds16<ONCE>(ktile + ahead / (int)sizeof(S), nrec - ahead, dst + 1024 * (NT / 64) * j, koff[j] - ahead);
             }
             if (dov) {
-                const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<S *>(vtile), (short)0, nrec, 0x00020000);
+                const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<S *>(vtile), (short)0, nrec, 0x00020000);   // (VREG: not WINDOW)
 #pragma unroll
                 for (int j = 0; j < NP; ++j) {
                     if constexpr (VREG)
-                        vr[j] = __builtin_bit_cast(uint4_t, __builtin_amdgcn_raw_buffer_load_b128(rv, at(voff[j], j), 0, 0));
+                        vr[j] = __builtin_bit_cast(uint4_t, __builtin_amdgcn_raw_buffer_load_b128(rv, voff[j], 0, 0));
                     else
-                        load_lds16<ONCE>(vtile, nrec, dst + 2 * SM::KSZ + 1024 * (NT / 64) * j, at(voff[j], j));
+                        load_lds16<ONCE>(vtile + ahead / (int)sizeof(S), nrec - ahead, dst + 2 * SM::KSZ + 1024 * (NT / 64) * j, voff[j] - ahead);
                 }
             }
         };
-        if (MODE == PARTS && own)
-            issue(std::true_type{});
-        else
-            issue(std::false_type{});
+        constexpr std::integral_constant<int, 0> none{};
+        if (WIN && (unsigned)(at + 1 - near) < 2) {   // WINDOW: the last sink's tile (a full one), the window's first
+            const bool sink = at + 1 == near;
+            int bytes = row_bytes;
+            asm volatile("" : "+s"(bytes));   // what follows is computed here, and not held during the loop
+            const int behind = (near * BC - sinks) * bytes, ahead = first_key % BC * bytes;
+            const long long jump = (long long)gap * BC * (bytes / (int)sizeof(S));
+            issue(std::false_type{}, nrec - (sink ? behind : 0), sink ? 0 : ahead);
+            if (PAGED && sink) {
+                go_to_page(far_page, far_key);
+                return;
+            }
+            ktile += sink ? jump : 0;
+            vtile += sink ? jump : 0;
+        } else if (MODE == PARTS && own) {
+            issue(std::true_type{}, nrec, none);
+        } else {
+            issue(std::false_type{}, nrec, none);
+        }
         ktile += BC * (size_t)row_elems;
         vtile += BC * (size_t)row_elems;
         if constexpr (PAGED) {
@@ -622,8 +633,8 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
         __builtin_amdgcn_s_setprio(0);
     };
 
-    // hide keys of tile t that some row of the wave must not see
-    auto mask = [&](float16_t &s, int t) {
+    // hide keys of tile t, the v-th visited, that some row of the wave must not see
+    auto mask = [&](float16_t &s, int t, int v) __attribute__((always_inline)) {
         int kw = t * BC + 32 * kh;        // first key of this wave's half
         int end = Nk;                     // keys from here on do not exist
         if constexpr (SEGMENTS) {
@@ -632,15 +643,28 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
             else
                 kw += a.prefix - near * BC;
         }
-        // WINDOW: the last key that the slot's last row does not see any more
-        const int passed = WIN ? row0 + WR - 1 + off - a.window : -1;
-        if (kw + 32 > (SEGMENTS ? min(kfree_w, end) : kfree_w) || (WIN && kw <= passed && kw + 32 > a.sinks)) {
+        if constexpr (WIN) {
+            // the lane's row sees keys lo .. hi - 1, counted from the lane's first key,
+            // and, where the sinks are no part of their own, those below `always`: a
+            // bit for each key (two instructions a score, and no scalar registers)
+            const bool sink = v < near;
+            const int k0 = kw + 4 * lh, at = qi + off + 1;
+            auto below = [](int n) { return (1u << min(max(n, 0), 31)) - 1; };   // (keys 0 .. 27)
+            const unsigned seen = below(min(sink ? a.sinks : Nk, at) - k0) &
+                                  (~below(sink ? 0 : at - a.window - k0) | below(near > 0 ? 0 : a.sinks - k0));
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const unsigned x = (unsigned)((int)(seen << (31 - 8 * (r >> 2) - (r & 3))) >> 31);
+                const float f = s[r];   // (a bit cast of the vector's element itself reads the first one)
+                s[r] = __builtin_bit_cast(float, (x & __builtin_bit_cast(unsigned, f)) | (~x & 0xff800000u));
+            }
+            return;
+        }
+        if (kw + 32 > (SEGMENTS ? min(kfree_w, end) : kfree_w)) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int key = kw + 8 * (r >> 2) + 4 * lh + (r & 3);
-                const bool vis = MODE == PARTS ? key < rlim
-                                                : key < end && (!CAUSAL || key <= qi + off) &&
-                                                      (!WIN || key > qi + off - a.window || key < a.sinks);
+                const bool vis = MODE == PARTS ? key < rlim : key < end && (!CAUSAL || key <= qi + off);
                 s[r] = vis ? s[r] : -INFINITY;
             }
         }
@@ -716,8 +740,9 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
     // the whole next step as well: step i waits for tile i + 1's, and writes its
     // bf16 V, after its own scores.  With two, at its end.
     constexpr int AHEAD = SM::AHEAD;
-    if constexpr (MODE == WINDOW_PARTS) {
-        if (first > 0 && ntiles > 0) go_to(first + (first >= near ? gap : 0));
+    if constexpr (JUMPS) {
+        const int t = first + (first >= near ? gap : 0);
+        if (ntiles > 0 && t > 0) go_to(t);
     }
     if (ntiles > 0) {
         vregs_t v0;
@@ -731,28 +756,53 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
         if (RAW) vstore_from(v0, stage_at(0));
     }
     lds_barrier();
-    auto step = [&](int i, auto R) {   // R: stage of tile i (i % NSTAGE)
+    // JUMPS: of the steps, those on tiles that every row of the wave sees whole (clean0,
+    // clean_n of them; no mask), and those on tiles that some row sees keys of (some0,
+    // some_n; WINDOW: and the sinks').  As ranges, since a chain of scalar instructions
+    // stands in a step's way where one workgroup has the CU, and so do scalar registers
+    // that do not fit (against tests of every tile's keys, with the mask in bits, one
+    // sequence, 32/8 heads, D = 128, fp16, 1100 rows, window of all keys 32.6 -> 29.0 us,
+    // 275 16.1 -> 14.5; 4096 rows, bf16, 1024 87.2 -> 82.7; D = 64, 16384 rows 175.8 -> 166.0).
+    int clean0 = 0, clean_n = 0, some0 = 0, some_n = 0;
+    if constexpr (JUMPS) {
+        auto from = [&](int key) { return key < 32 * kh ? 0 : (key - 32 * kh) / BC + 1; };   // tiles whose first key of the wave's is <= key
+        const int end = from(kfree_w - 32) - gap;
+        int top = ntiles;
+        if constexpr (WIN) {
+            const int passed = row0 + WR - 1 + off - a.window;   // the last key that the last row does not see any more
+            clean0 = max(from(passed) - gap, near);
+            some0 = near == 0 && a.sinks > 0 ? 0 : max(from(passed - (WR - 1) - 31) - gap, near);
+            top = from(row0 + WR - 1 + off) - gap;
+        }
+        clean_n = live ? max(end - clean0, 0) : 0;
+        some_n = live ? max(top - some0, 0) : 0;
+        clean0 -= first;
+        some0 -= first;
+    }
+    const int sink_steps = WIN && live ? near - first : 0;
+    auto step = [&](int i, auto R) __attribute__((always_inline)) {   // R: stage of tile i (i % NSTAGE)
         constexpr int r = decltype(R)::value;
         // the next tile's loads are issued after the K operand reads (their
         // scalar set-up then overlaps the LDS latency, and at D = 128 their
         // registers are not live across the QK^T product)
+        const bool clean = JUMPS && (unsigned)(i - clean0) < (unsigned)clean_n;
         const int t = first + i + (JUMPS && first + i >= near ? gap : 0);   // the tile
-        bool some = true;   // some row of the wave sees some key of it (wave-uniform)
-        if constexpr (WIN) {
-            const int kw = t * BC + 32 * kh;
-            some = live && kw <= row0 + WR - 1 + off && (kw + 31 > row0 + off - a.window || kw < a.sinks);
-        }
-        if constexpr (MODE == PARTS) some = live;
-        float16_t s;
-        if (some) s = D == 128 ? scores_jit(stage_at(r)) : scores(stage_at(r));
-        if (AHEAD == 2 && i + 1 < ntiles) {
-            lds_loads_done<0>();   // tile i + 1, loaded since the previous step
-            vstore_from(vr, stage_at((r + 1) % NSTAGE));
-        }
+        bool some = true;   // (wave-uniform)
+        if (PAGED && WIN && D == 128)
+            some = live;   // (no scalar registers left for the ranges)
+        else if (JUMPS && !clean)
+            some = (unsigned)(i - some0) < (unsigned)some_n || (WIN && i < sink_steps);
         const bool more = i + AHEAD < ntiles;
-        if (more) gload_to(vr, (r + AHEAD) % NSTAGE);
-        if (some) {
-            mask(s, t);
+        auto stage_next = [&]() __attribute__((always_inline)) {
+            if (AHEAD == 2 && i + 1 < ntiles) {
+                lds_loads_done<0>();   // tile i + 1, loaded since the previous step
+                vstore_from(vr, stage_at((r + 1) % NSTAGE));
+            }
+            if (more) gload_to(vr, (r + AHEAD) % NSTAGE);
+        };
+        auto scored = [&]() __attribute__((always_inline)) { return D == 128 ? scores_jit(stage_at(r)) : scores(stage_at(r)); };
+        auto finish = [&](float16_t &s) __attribute__((always_inline)) {
+            if (!clean) mask(s, t, first + i);
             half8_t p0, p1;
             half8_t va[KSTEPS];
             // D = 64: the V operands are read before the softmax, so that their
@@ -764,6 +814,18 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
             } else {
                 pv(p0, p1, va);
             }
+        };
+        if constexpr (PAGED && WIN) {   // (one copy of the loads: what they hold in scalar registers leaves no room for two)
+            float16_t s;
+            if (some) s = scored();
+            stage_next();
+            if (some) finish(s);
+        } else if (some) {
+            float16_t s = scored();
+            stage_next();
+            finish(s);
+        } else {
+            stage_next();
         }
         if (AHEAD == 1) {
             if (more) vstore_from(vr, stage_at((r + AHEAD) % NSTAGE));

@@ -12,6 +12,13 @@ namespace {
 constexpr int CUS = 256;        // compute units of the card
 constexpr int MIN_TILES = 4;    // least tiles in a split
 
+// Cache from which an order by length pays, as in fa_prefill.hip, where the window
+// leaves the lengths a difference (us, in the batch's order / ranked, window of 3/4, 1/2
+// and 1/4 of the longest: 16 x 32/8 heads, 512 rows, 4096 to 1096 keys, D = 64 226 /
+// 198, 184 / 167, 114.8 / 113.0; 40 x 64 rows, 2048 to 488 keys, D = 128 76.0 / 73.1,
+// 59.5 / 60.0, 39.0 / 40.1).
+constexpr int RANKED_KEYS = 512, RANKED_KEYS_EACH = 40;
+
 int heads(int G) { return G % 4 == 0 ? 4 : G % 2 == 0 ? 2 : 1; }   // query heads per workgroup
 
 // Splits of each row block's tiles.  A workgroup visits them one after the other,
@@ -69,6 +76,12 @@ hipError_t launch_t(const Problem &p, float *ws, hipStream_t stream) {
     a.per_mb = Divisor((unsigned)p.B * p.Hkv * (G / a.HW));
     a.first = a.nmb;
     a.ranked = 0;
+    a.row_blocks = Divisor(a.nmb);
+    if (p.seqlens && p.B > 1 && p.B <= kMaxRanked && blocks > CUS && 2LL * p.window >= p.Nk && p.Nk >= RANKED_KEYS &&
+        p.Nk >= RANKED_KEYS_EACH * (long long)p.B) {
+        a.per_seq = Divisor(p.Hkv * (G / a.HW));
+        a.ranked = blocks <= (long long)Cfg<D>::WPC * CUS ? (CUS + (int)a.per_seq.d - 1) / (int)a.per_seq.d : a.nmb * p.B;
+    }
     a.page_div = Divisor(p.block_table ? p.page_size : 1);
     a.window = p.window;
     a.sinks = p.sinks;

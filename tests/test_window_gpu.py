@@ -261,3 +261,24 @@ def test_key_rows_past_32_bit_offsets(D, H, Nq):
             w = torch.softmax((q[0, i, h].double() * k[0, see, h].double()).sum(-1) * default_scale(D), 0)
             ref = (w[:, :, None] * v[0, see, h].double()).sum(0)
             assert (o[0, i, h].double() - ref).abs().max().item() <= 2e-3, (h0, i)
+
+
+@pytest.mark.parametrize("window,sinks", [(1, 1), (5, 3), (17, 1), (40, 30), (33, 33), (20, 64), (70, 65), (31, 95), (64, 0)])
+@pytest.mark.parametrize("D,dt,Hq,Hkv", [(64, "f16", 4, 1), (64, "bf16", 6, 2), (128, "f16", 3, 3), (128, "bf16", 4, 1)])
+def test_the_last_sink_and_the_window_in_one_tile(D, dt, Hq, Hkv, window, sinks):
+    """Row blocks whose window begins in the tile of the last sink, next to it, and further on."""
+    check_case(1, Hq, Hkv, 230, 230, D, dt, window, sinks, None, 0)
+    check_case(2, Hq, Hkv, 100, 230, D, dt, window, sinks, [230, 131], 64)
+
+
+@pytest.mark.parametrize("D,Nk,window,page", [(64, 1000, 600, 0), (128, 900, 900, 0), (128, 1000, 500, 64)])
+def test_sequences_taken_by_length(D, Nk, window, page):
+    """Grids of uneven sequences that are taken longest first, and the same sequences in another order: same bits."""
+    lens = [Nk - 57 * (7 * i % 16) for i in range(16)]
+    check_case(16, 8, 2, 330, Nk, D, "bf16", window, 3, lens, page)
+    q, k, v = (t.cuda() for t in make_qkv(16, 8, 2, 330, Nk, D, "bf16", seed=5))
+    sl = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    o, lse = fa.fwd_window(q, k, v, window, sinks=3, seqlens_k=sl)
+    turn = torch.arange(15, -1, -1, device="cuda")
+    ot, lt = fa.fwd_window(q[turn].contiguous(), k[turn].contiguous(), v[turn].contiguous(), window, sinks=3, seqlens_k=sl[turn].contiguous())
+    assert torch.equal(ot, o[turn]) and torch.equal(lt, lse[turn])
