@@ -640,7 +640,11 @@ hipError_t launch_t(const Problem &p, hipStream_t stream) {
 //     +26 %) and where a causal call's longest row block then decides (bf16, D =
 //     256, 32/8 x 1024 45.6 / 59.5, x 1371 80.6 / 77.3, x 1718 110 / 94)
 // With a window all rows but the first take about the same time, so that a causal
-// call's second half is no shorter, and a long chain of steps is rare:
+// call's second half is no shorter, and a long chain of steps is rare (from a window of
+// 3/4 of the keys on the lines above hold: with them, windows of all keys, 3/4 and 1/2,
+// fp32, 14/2 heads, 777 rows, D = 64 26.7 -> 23.2, 23.8 -> 22.2, 21.6 -> 21.3; 32/8 x 500
+// 23.7 -> 23.3, 21.7 -> 23.0, 17.8 -> 22.3; fp16, 32/8 x 700, D = 80 19.0 -> 16.9, 19.3 ->
+// 17.2, 15.9 -> 16.9; bf16, 16/2 x 1111, D = 96 23.5 -> 21.6, 21.1 -> 20.3, 16.7 -> 16.9):
 //   16 bits, (4, 2) past the line of (2, 4) at once: 16/2 x 1280 rows, window 300,
 //     D = 96 13.9 against 19.0 with (2, 2) and 23.0 with (2, 4)
 //   fp32 up to 128 columns, past the line of (1, 4): (2, 2) for windows of up to 512
@@ -660,9 +664,10 @@ hipError_t launch_k(const Problem &p, hipStream_t s) {
     } else if constexpr (F32 || !WIDE) {
         constexpr int NS = F32 && !WIDE ? 1 : 2, KSP = WIDE ? 2 : 4;
         constexpr int FIT = 163840 / GCfg<TIN, DP, NS, KSP, NB>::BYTES;   // workgroups per CU by LDS
-        const int rounds = !WIN && p.causal && p.Nk < 2LL * p.Nq ? 2 : 1;
+        const bool all = !WIN || 4LL * p.window >= 3LL * p.Nk;
+        const int rounds = all && p.causal && p.Nk < 2LL * p.Nq ? 2 : 1;
         if (groups(NS) <= CUS * (FIT < 2 ? FIT : 2) * rounds) return launch_t<TIN, TOUT, DP, NS, KSP, NB, WIN>(p, s);
-        if constexpr (!WIN && !F32 && DP == 96) {
+        if constexpr (!F32 && DP == 96) {
             constexpr int FIT2 = 163840 / GCfg<TIN, DP, 2, 2, NB>::BYTES;
             if (rounds == 2 && groups(2) <= CUS * FIT2) return launch_t<TIN, TOUT, DP, 2, 2, NB, WIN>(p, s);
         }

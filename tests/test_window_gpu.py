@@ -282,3 +282,10 @@ def test_sequences_taken_by_length(D, Nk, window, page):
     turn = torch.arange(15, -1, -1, device="cuda")
     ot, lt = fa.fwd_window(q[turn].contiguous(), k[turn].contiguous(), v[turn].contiguous(), window, sinks=3, seqlens_k=sl[turn].contiguous())
     assert torch.equal(ot, o[turn]) and torch.equal(lt, lse[turn])
+
+
+@pytest.mark.parametrize("Hq,Hkv,N,D,dt", [(14, 2, 777, 64, "f32"), (16, 2, 1111, 96, "bf16"), (32, 8, 300, 80, "f16")])
+def test_long_windows_of_other_head_sizes(Hq, Hkv, N, D, dt):
+    """Windows of most of the keys take the workgroup layouts of causal calls."""
+    for window in (N, N * 3 // 4, N * 3 // 4 - 20):
+        check_case(1, Hq, Hkv, N, N, D, dt, window, 2, None, 0)
