@@ -355,12 +355,14 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
         koff[j] = r * row_bytes + 16 * (c ^ kswz(r));
         voff[j] = r * row_bytes + 16 * (c ^ vswz(r));
     }
-    // WINDOW, PARTS (and WINDOW_PARTS): bf16 V also goes to LDS directly, as it is, and becomes fp16 in its
-    // place once it is there, so that no registers hold it during a step (window
-    // 1024, 32/8 heads, D = 128, bf16: 4096 rows 90.1 -> 85.1 us, 8192 168.6 -> 160.8; with
-    // five stages instead of three, and two waves per SIMD, 91.8 and 177.8; JOIN, 8 x
-    // 256 rows behind 4096 + 512 keys, 157.8 against 154.2 through registers).
-    constexpr bool RAW = IN_BF16 && JUMPS, VREG = IN_BF16 && !RAW;
+    // PARTS, paged WINDOW: bf16 V also goes to LDS directly, as it is, and becomes fp16 in
+    // its place once it is there.  A paged window has no registers left to hold it during
+    // a step (29 would spill); PARTS takes less time so where its grid is full (64 x 32/8
+    // heads behind 8192 keys 43.5 us against 49.0 through registers; 8 x 8 rows 24.5
+    // against 23.2).  Contiguous windows have them (32/8 heads, D = 128, 4096 rows, window
+    // 1024 80.5 us against 82.7 by way of LDS), and so has JOIN (8 x 256 rows behind 4096 +
+    // 512 keys 154.2 against 157.8).
+    constexpr bool RAW = IN_BF16 && (MODE == PARTS || (WIN && PAGED)), VREG = IN_BF16 && !RAW;
     typedef uint4_t vregs_t[VREG ? NP : 1];
     vregs_t vr;   // bf16: the next tile's V chunks, in flight during a step
     // Scalar state of the next tile to load: the address of its first key row
@@ -464,11 +466,11 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
                     load_lds16<ONCE>(ktile + ahead / (int)sizeof(S), nrec - ahead, dst + 1024 * (NT / 64) * j, koff[j] - ahead);
             }
             if (dov) {
-                const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<S *>(vtile), (short)0, nrec, 0x00020000);   // (VREG: not WINDOW)
+                const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<S *>(vtile + ahead / (int)sizeof(S)), (short)0, nrec - ahead, 0x00020000);
 #pragma unroll
                 for (int j = 0; j < NP; ++j) {
                     if constexpr (VREG)
-                        vr[j] = __builtin_bit_cast(uint4_t, __builtin_amdgcn_raw_buffer_load_b128(rv, voff[j], 0, 0));
+                        vr[j] = __builtin_bit_cast(uint4_t, __builtin_amdgcn_raw_buffer_load_b128(rv, voff[j] - ahead, 0, 0));
                     else
                         load_lds16<ONCE>(vtile + ahead / (int)sizeof(S), nrec - ahead, dst + 2 * SM::KSZ + 1024 * (NT / 64) * j, voff[j] - ahead);
                 }
