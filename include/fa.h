@@ -488,6 +488,9 @@ size_t fa_window_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Nk, int D, 
  * The Nq queries of sequence b are the last Nq of its Np + seqlens_k[b] positions;
  * with causal = 1 query i sees its first i + 1 + Np + seqlens_k[b] - Nq keys (a row
  * that sees none gives 0 and -inf).  fp16 / bf16 with D in {64, 128}.
+ * Keys past a sequence's length may hold anything, also infinities and NaN; keys
+ * that some query of the call sees must be finite, since the others' weight of 0
+ * times an infinite value is NaN.
  * workspace, workspace_bytes: device scratch of this call
  * (fa_prefix_workspace_bytes), 16-byte aligned, or NULL and 0: the library's or
  * the one that is set (see the top); calls that need none ignore it.  Graphs
@@ -505,12 +508,14 @@ fa_status_t fa_fwd_prefix(const void *q, const void *k_prefix, const void *v_pre
                           size_t workspace_bytes);
 
 /* fa_fwd_prefix against the paged cache of fa_fwd_kvcache_paged, the arguments
- * and the result of that call (lengths count the prefix; a sequence may be
- * shorter than it): the first prefix_len keys of all sequences are in the same
- * pages, and every row of the table names them.  prefix_len: a positive multiple
+ * and the result of that call (lengths count the prefix; a sequence, or all of
+ * them, may be shorter than it: what lies behind the longest one may hold
+ * anything): the first prefix_len keys of all sequences are in the same pages, and
+ * every row of the table names them.  prefix_len: a positive multiple
  * of page_size, at most page_size * max_pages.  Workspace:
  * fa_prefix_workspace_bytes with Np = prefix_len, Nk = page_size * max_pages -
- * prefix_len.  Errors: FA_ERR_DIM for another prefix_len; otherwise those of fa_fwd_prefix and fa_fwd_kvcache_paged. */
+ * prefix_len.  Errors: FA_ERR_DIM for another prefix_len; otherwise those of
+ * fa_fwd_prefix and fa_fwd_kvcache_paged. */
 fa_status_t fa_fwd_prefix_paged(const void *q, const void *k_pages, const void *v_pages, void *o,
                                 float *lse, const int *seqlens_k, const int *block_table, int B,
                                 int Hq, int Hkv, int Nq, int D, int page_size, int max_pages,

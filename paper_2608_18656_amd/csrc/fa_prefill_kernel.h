@@ -167,6 +167,16 @@ __device__ __forceinline__ int own_keys(const PrefillArgs &a, int b) {
     return a.seqlens ? min(max(min(max(a.seqlens[b], 0), a.prefix + a.own) - a.counted, 0), a.own) : a.own;
 }
 
+// Keys of the prefix that a row sees (PARTS): fewer than all where it lies in the
+// prefix (causal), or its sequence is shorter.
+__device__ __forceinline__ int prefix_keys(const PrefillArgs &a, int row) {
+    const int t = a.group.div(row), b = a.tokens.div(t);
+    int n = a.prefix + a.own;
+    if (a.seqlens) n = min(min(max(a.seqlens[b], 0), n) + a.prefix - a.counted, n);
+    if (a.causal) n += t - b * a.Nq + 1 - a.Nq;
+    return min(max(n, 0), a.prefix);
+}
+
 template <typename TIN, typename TOUT, int D, int NS, bool CAUSAL, bool PAGED, int MODE = ALL>
 __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_eu((Cfg<D, NS>::WPE), (Cfg<D, NS>::WPE)))) void prefill_kernel(PrefillArgs a) {
     using S = typename TIN::scalar;
@@ -259,9 +269,23 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
     // Valid keys of this batch element: with per-sequence lengths the K/V
     // tensors hold a.Nk rows per batch element of which the first seqlens[b]
     // are valid, and the queries are the sequence's last Nq positions.
-    // PARTS: of the part: the prefix's or the sequence's own.  JOIN: of both.
+    // PARTS: of the part: the sequence's own, or of the prefix those that some row
+    // of the workgroup sees: what lies behind the longest sequence is not read, and
+    // may hold anything.  JOIN: of both.
     int valid = min(max(len, 0), a.Nk);
-    if constexpr (MODE == PARTS) valid = own ? own_keys(a, b0) : a.prefix;
+    if constexpr (MODE == PARTS) {
+        valid = own ? own_keys(a, b0) : a.prefix;
+        if (!own && (a.causal || a.counted)) {
+            static_assert(WR * NSLOT == 128, "two rows a lane");
+            const int row = row0_wg + l;
+            int n = max(prefix_keys(a, min(row, Nq - 1)), prefix_keys(a, min(row + 64, Nq - 1)));
+            if (__builtin_amdgcn_ballot_w64(n == a.prefix) == 0) {
+#pragma unroll
+                for (int x = 32; x > 0; x >>= 1) n = max(n, __shfl_xor(n, x));
+                valid = n;
+            }
+        }
+    }
     if constexpr (SEGMENTS) valid = a.prefix + own_keys(a, b);
     const int Nk = __builtin_amdgcn_readfirstlane(valid);
     const int off = Nk - Nq;
@@ -300,14 +324,11 @@ __global__ __launch_bounds__((Cfg<D, NS>::NT)) __attribute__((amdgpu_waves_per_e
         const int each = (ntiles + nsplit - 1) / nsplit;
         gap = min(split * each, ntiles);
         ntiles = min(ntiles - gap, each);
-        const int sb = a.tokens.div(tok), i = tok - sb * a.Nq;
         rlim = Nk;
         if (own) {
-            if (a.causal) rlim = min(Nk - a.Nq + i + 1, Nk);
+            if (a.causal) rlim = min(Nk - a.Nq + (tok - (int)a.tokens.div(tok) * a.Nq) + 1, Nk);
         } else if (a.causal || a.counted) {   // rows that lie in the prefix, sequences shorter than it
-            int n = a.prefix + a.own;
-            if (a.seqlens) n = min(min(max(a.seqlens[sb], 0), n) + a.prefix - a.counted, n);
-            rlim = a.causal ? min(n - a.Nq + i + 1, Nk) : min(n, Nk);
+            rlim = prefix_keys(a, min(qi, Nq - 1));
         }
         // some row does not see all of the part: every tile is masked
         if (__builtin_amdgcn_ballot_w64(rlim < Nk)) kfree_w = 0;
