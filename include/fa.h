@@ -53,6 +53,9 @@
  *    after the stream is destroyed, again until fa_release_workspace());
  *  - fa_set_workspace() installs one caller-owned buffer for a device, which
  *    then serves every call on that device that does not pass its own.
+ * A call that uses a shared buffer (the library's, the one that is set, the fixed
+ * array of fa_fwd_splitkv_noalloc) enqueues all its kernels before another such
+ * call does, so that several host threads may call on one stream at a time.
  */
 #ifndef FA_H_
 #define FA_H_

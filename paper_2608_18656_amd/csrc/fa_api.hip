@@ -42,13 +42,17 @@ struct UserWs {
 UserWs g_user[kMaxDevices];
 std::vector<OwnedWs> g_owned;
 std::vector<Retired> g_retired;
+// Guards these, and is held by a call that uses one of the buffers until all of its
+// kernels are enqueued: another host thread's call on the same stream must not come
+// between the kernel that leaves partial results and the one that merges them, nor
+// a release between the choice of a buffer and its use.
 std::mutex g_ws_mu;
 
 // need: what the call uses; room: what a new buffer holds (for shorter caches too).
+// With g_ws_mu held.
 fa_status_t get_workspace(size_t need, size_t room, hipStream_t stream, void **out, bool *user) {
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return FA_ERR_HIP;
-    std::lock_guard<std::mutex> lk(g_ws_mu);
     *user = g_user[dev].ptr != nullptr;
     if (*user) {
         if (g_user[dev].bytes < need) return FA_ERR_WORKSPACE;
@@ -109,14 +113,13 @@ struct CallWs {
 constexpr size_t kScratchBytes = (size_t)32 << 20;
 static __device__ __align__(256) unsigned char scratch[kScratchBytes];
 void *g_scratch_ptr[kMaxDevices];
-std::mutex g_scratch_mu;
+std::mutex g_scratch_mu;   // guards these, and is held until a call's kernels are enqueued
 
 // Device address of the current device's scratch (read on the first call per
-// device, with that device current).
+// device, with that device current).  With g_scratch_mu held.
 fa_status_t scratch_address(void **out) {
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return FA_ERR_HIP;
-    std::lock_guard<std::mutex> lk(g_scratch_mu);
     if (!g_scratch_ptr[dev]) {
         void *ptr = nullptr;
         if (hipGetSymbolAddress(&ptr, HIP_SYMBOL(scratch)) != hipSuccess || ptr == nullptr) {
@@ -187,6 +190,7 @@ fa_status_t run(const void *q, const void *k, const void *v, void *o, float *lse
         room = fa::window_workspace_bytes(B, Hq, Hkv, Nq, Nk, D, p.window, p.sinks, true);
     }
     void *ws = nullptr;
+    std::unique_lock<std::mutex> lock(g_ws_mu, std::defer_lock);
     if (need > 0) {
         bool user = false;
         if (cws) {   // this call's own workspace: checked here, never allocated
@@ -196,6 +200,7 @@ fa_status_t run(const void *q, const void *k, const void *v, void *o, float *lse
             ws = cws->ptr;
             user = true;
         } else {
+            lock.lock();
             st = get_workspace(need, room, s, &ws, &user);
             if (st != FA_OK) return st;
         }
@@ -370,6 +375,7 @@ fa_status_t prefix(const void *q, const void *k_prefix, const void *v_prefix, co
     const size_t need = fa::prefix_workspace_bytes(B, Hq, Hkv, Nq, Np, Nk, D, false);
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     bool user = workspace || workspace_bytes;
+    std::unique_lock<std::mutex> lock(g_ws_mu, std::defer_lock);
     if (need == 0) {   // one pass: no workspace
         user = false;
     } else if (user) {
@@ -377,6 +383,7 @@ fa_status_t prefix(const void *q, const void *k_prefix, const void *v_prefix, co
         if (fa::misaligned(workspace, 16)) return FA_ERR_ALIGN;
         if (workspace_bytes < need) return FA_ERR_WORKSPACE;
     } else {
+        lock.lock();
         st = get_workspace(need, fa::prefix_workspace_bytes(B, Hq, Hkv, Nq, Np, Nk, D, true), s, &workspace, &user);
         if (st != FA_OK) return st;
     }
@@ -480,9 +487,11 @@ fa_status_t fa_fwd_splitkv_noalloc(const void *q, const void *k, const void *v, 
     if (st != FA_OK) return st;
     if (num_splits < 0 || num_splits > FA_MAX_SPLITS) return FA_ERR_SPLITS;
     CallWs cws{nullptr, 0};
+    std::unique_lock<std::mutex> lock(g_scratch_mu, std::defer_lock);
     if (fa::decode_supported(Nq, Hkv, D, in_dtype)) {
         const int S = num_splits > 0 ? num_splits : fa::decode_default_splits(B, Hq, Hkv, Nk, D);
         if (fa::decode_workspace_bytes(B, Hq, D, S) > kScratchBytes) return FA_ERR_WORKSPACE;
+        lock.lock();
         st = scratch_address(&cws.ptr);
         if (st != FA_OK) return st;
         cws.bytes = kScratchBytes;
