@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import operator
 
 from . import _lib
 
@@ -447,7 +448,10 @@ def _rotary(rt, inv_freq, positions, pair_axes, interleaved, B, N, index):
         if pair_axes is None or len(pair_axes) != pairs:
             raise ValueError("several axes need pair_axes, the axis of each of the rot_dim / 2 pairs")
         if pairs <= _lib.FA_MAX_ROTARY_PAIRS:   # (more are refused by the call)
-            ctypes.memmove(r.pair_axis, bytes(pair_axes), pairs)
+            # item by item: bytes() of an array of wider integers is its memory
+            if not isinstance(pair_axes, bytes):
+                pair_axes = bytes(operator.index(a) for a in pair_axes)
+            ctypes.memmove(r.pair_axis, pair_axes, pairs)
     return r
 
 
@@ -518,8 +522,8 @@ def kvcache_append(k, v, k_cache, v_cache, seqlens_k, q=None, q_out=None, inv_fr
     stride between tokens).  ``inv_freq`` (float32 [rot_dim / 2], None: no
     rotation): radians per position of each pair of columns, j and j + rot_dim /
     2, or 2 j and 2 j + 1 if ``interleaved``.  ``positions``: int32 [B, N], or
-    [axes, B, N] with ``pair_axes``, the axis that turns each pair (bytes or a
-    sequence of ints); None: the cache rows.  Returns the rotated queries
+    [axes, B, N] with ``pair_axes``, the axis that turns each pair (bytes or any
+    sequence of integers); None: the cache rows.  Returns the rotated queries
     (``q_out`` if given, which may be ``q`` if that is contiguous; None without
     ``q``)."""
     return _append(k, v, k_cache, v_cache, None, seqlens_k, q, q_out, inv_freq, positions, pair_axes, interleaved)
