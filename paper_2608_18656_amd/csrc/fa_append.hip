@@ -24,12 +24,14 @@ namespace {
 
 constexpr int NT = 256;           // threads per workgroup
 constexpr int MAX_PAIRS = 128;    // D <= 256
-// Bytes up to which the inputs are read through the caches.  A projection leaves its
-// result in the memory side's 256 MB, from where plain loads are quicker (5777
-// tokens, 16/2 heads, D = 128, 59 MB: 11.9 us, non-temporal 13.8); a long prompt's does
-// not stay there with what is written (8192 tokens, 32/8 heads, D = 128, 201 MB: 42.3
-// us, non-temporal 34.8; 131 MB 28.0 / 26.5).
-constexpr long long HELD = 128 << 20;
+// Bytes read and written up to which the inputs are read through the caches.  A
+// projection leaves its result in the memory side's 256 MB, from where plain loads are
+// quicker; a long prompt's does not stay there with what is written.  32/8 heads, D =
+// 128, fp16, us with plain / non-temporal loads, right behind a kernel that writes the
+// inputs: 73 MB 14.4 / 15.2, 88 16.7 / 16.6, 103 19.1 / 19.0, 131 23.1 / 23.4, 147 25.6 /
+// 26.2, 172 31.7 / 29.2, 201 36.8 / 35.7; three sets in turn: 73 MB 14.9 / 18.7, 88 20.3
+// / 20.2, 103 24.8 / 23.5, 131 31.9 / 27.7, 201 46.1 / 41.3.
+constexpr long long HELD = 96 << 20;
 
 struct AppendArgs {
     const void *q, *k, *v;
@@ -170,7 +172,10 @@ __global__ __launch_bounds__(NT) void append_kernel(AppendArgs a) {
                     *reinterpret_cast<V *>(dst + E * c) = x[n];
                 }
             }
-        } else {   // unit u: a pair, or two of the columns past the rotated ones
+        } else {
+            // unit u: a pair, or two of the columns past the rotated ones, element by
+            // element (8192 tokens, 32/8 heads, fp16: 20 of 128 columns rotated 66.7 us, all
+            // of them 43.6; 24 of 96 in halves 52.9, as neighbours in chunks 36.6)
             const int i0 = 2 * u < rot && !a.interleaved ? u : 2 * u, i1 = 2 * u < rot && !a.interleaved ? u + rot / 2 : 2 * u + 1;
             S x = src[i0], y = src[i1];
             if (2 * u < rot) {
