@@ -138,18 +138,16 @@ struct Window {
 };
 
 // Splits of a decode call, and the most of any shorter cache.  With a window they
-// go by the keys that it leaves.  Up to ONE_SPLIT of those at D = 64 one split is as
-// quick as several and their merge, and saves the second launch (1028 keys, one
-// sequence, 32/8 heads: 10.3 us a call against 12.7 among others, 24.9 against 24.3
-// waited for; 2052 keys 16.8 against 12.8; D = 128, 516 keys 26.3 against 25.1 waited
-// for).
-constexpr int ONE_SPLIT = 1152;
+// go by the keys that it leaves, as for a cache of that length: one split would save
+// the merge's launch, and with it 2 to 3 us of the host's time a call, but costs the
+// GPU more (32/8 heads, D = 64, one sequence, caches that nothing holds, us replayed
+// from a graph / waited for, several splits against one: 512 keys, one by the model,
+// 7.3 / 23.3; 640 7.4 / 24.2 against 8.2 / 25.1, 768 7.6 / 24.5 against 9.2 / 25.7, 1024
+// 7.7 / 24.6 against 10.9 / 27.4; 16/1 heads, 640 6.7 / 23.1 against 6.5 / 23.1, 768 7.0 /
+// 23.7 against 7.0 / 23.4, 1024 7.0 / 23.5 against 8.0 / 24.0).
 int decode_splits(int B, int Hq, int Hkv, int Nk, int D, const Window &w, bool most) {
     long long keys = Nk;
-    if (w.size > 0) {
-        if ((long long)w.size + w.sinks < keys) keys = (long long)w.size + w.sinks;
-        if (D == 64 && keys <= ONE_SPLIT) return 1;
-    }
+    if (w.size > 0 && (long long)w.size + w.sinks < keys) keys = (long long)w.size + w.sinks;
     return most ? fa::decode_most_splits(B, Hq, Hkv, (int)keys, D) : fa::decode_default_splits(B, Hq, Hkv, (int)keys, D);
 }
 
