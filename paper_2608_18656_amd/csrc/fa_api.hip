@@ -151,6 +151,15 @@ int decode_splits(int B, int Hq, int Hkv, int Nk, int D, const Window &w, bool m
     return most ? fa::decode_most_splits(B, Hq, Hkv, (int)keys, D) : fa::decode_default_splits(B, Hq, Hkv, (int)keys, D);
 }
 
+// Most keys of a call: the kernels count keys in ints, up to the end of the last tile of
+// at most 128, and a tile ahead.  Without a window the decode kernel has no such end,
+// and pages, 64 keys at least, end 64 ahead of 2^31: enough for the 16-bit kernels' tiles.
+constexpr int kMostKeys = 0x7fffffff - 255;
+bool keys_fit(int Nk, bool decode, bool prefill, bool paged, bool windowed) {
+    if (Nk <= kMostKeys) return true;
+    return paged ? decode || prefill : decode && !windowed;
+}
+
 struct Paging {
     const int *block_table = nullptr;
     int page_size = 0, max_pages = 0, num_pages = 0;
@@ -176,6 +185,7 @@ fa_status_t run(const void *q, const void *k, const void *v, void *o, float *lse
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     const bool decode = fa::decode_supported(Nq, Hkv, D, in), prefill = fa::prefill_supported(Hkv, D, in);
     const bool windowed = win.size > 0;
+    if (!keys_fit(Nk, decode, prefill, pg.block_table != nullptr, windowed)) return FA_ERR_DIM;
     // partial results: bytes that the call uses, and that a new buffer holds
     int S = 1;
     size_t need = 0, room = 0;
@@ -255,7 +265,10 @@ int fa_version(void) { return (0 << 16) | (1 << 8) | 0; }
 fa_status_t fa_validate(const void *q, const void *k, const void *v, const void *o,
                         const float *lse, int B, int Hq, int Hkv, int Nq, int Nk, int D,
                         int causal, float scale, fa_dtype_t in, fa_dtype_t out) {
-    return validate_core(q, k, v, o, lse, B, Hq, Hkv, Nq, Nk, D, causal, scale, in, out, -1);
+    const fa_status_t st = validate_core(q, k, v, o, lse, B, Hq, Hkv, Nq, Nk, D, causal, scale, in, out, -1);
+    if (st != FA_OK) return st;
+    return keys_fit(Nk, fa::decode_supported(Nq, Hkv, D, in), fa::prefill_supported(Hkv, D, in), false, false) ? FA_OK
+                                                                                                              : FA_ERR_DIM;
 }
 
 fa_status_t fa_fwd(const void *q, const void *k, const void *v, void *o, float *lse, int B,
