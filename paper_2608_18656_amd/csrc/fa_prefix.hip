@@ -29,7 +29,7 @@ constexpr int ROWS = WR * NSLOT;         // rows of a workgroup against the pref
 // workgroup, whose results are merged through LDS (WPR; a chain of loads the
 // fewer for the long lists that few rows have: 2 x 32/4 heads, 64 parts, 16.5 -> 13.7
 // us a call).
-constexpr int LONG_LIST = 16;   // parts from which four waves share a row
+constexpr int LONG_LIST = 16;   // most parts that one wave takes
 
 template <typename TOUT, int D, int WPR>
 __global__ __launch_bounds__(256) void merge_kernel(const float *__restrict__ opart, const float *__restrict__ mpart,
