@@ -38,9 +38,11 @@
  * before any HIP call; device faults surface at the caller's next
  * synchronisation.  No exception crosses this interface.
  *
- * Decode needs a device workspace for the per-split partial results
- * (fa_workspace_bytes()).  There are three ways to provide it:
- *  - the *_ws entry points take it with each call (caller-owned, checked
+ * Decode, windows and prefixes need a device workspace for partial results
+ * (fa_workspace_bytes(), fa_window_workspace_bytes(), fa_prefix_workspace_bytes()).
+ * There are three ways to provide it:
+ *  - the *_ws entry points, and those of windows and prefixes, take it with each
+ *    call (caller-owned, checked
  *    before any HIP call, never allocated by the library): calls running
  *    concurrently on different streams each pass their own;
  *  - otherwise the library owns one buffer per (device, stream), allocated on
@@ -431,7 +433,8 @@ fa_status_t fa_kvcache_append(const void *k, const void *v, void *k_cache, void 
  * A token whose table entry lies outside [0, num_pages) is not written, nor is
  * one past page_size * max_pages rows; the pages that a call writes to must be
  * the tokens' own (two tokens that name one row leave either's values there).
- * fp16, bf16 and fp32, any D that fa_kvcache_append takes.  Errors: those of
+ * fp16, bf16 and fp32, any D that fa_kvcache_append takes (the attention calls
+ * read pages of fp16 or bf16 with D of 64 or 128).  Errors: those of
  * fa_kvcache_append, FA_ERR_NULL for a NULL table, FA_ERR_DIM for page_size not a
  * positive multiple of 64, max_pages or num_pages < 1 or page_size * max_pages
  * or B * max_pages above 2^31 - 1. */

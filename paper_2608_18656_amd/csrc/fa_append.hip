@@ -13,8 +13,8 @@
 // row, those whose columns rotate together (both halves of the rotated columns,
 // or any two chunks where pairs are neighbours), so that it writes exactly what
 // it has read, and a rotation in place needs no barrier.
-// What bounds it: HBM for long prompts (8192 tokens, 32/8 heads, D = 128, fp16: 34.8
-// us, 5.8 TB/s read and written; a large copy reaches 5.0), the chain launch,
+// What bounds it: HBM for long prompts (8192 tokens, 32/8 heads, D = 128, fp16: 34.8 to
+// 37.6 us, 5.4 to 5.8 TB/s read and written; a large copy reaches 5.0), the chain launch,
 // lengths, table entry, store for a step of single tokens (64: 4.2 us).
 #include "fa_common.h"
 #include "fa_internal.h"
