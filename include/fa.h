@@ -83,8 +83,8 @@ typedef enum FA_ENUM_BASE {
 typedef enum FA_ENUM_BASE {
     FA_OK = 0,
     FA_ERR_NULL = 1,         /* q, k, v or o is NULL */
-    FA_ERR_DIM = 2,          /* a size is < 1, an index would overflow int64, or Nk is above 2^31 - 256 (but in
-                              * decode without a window, and in pages of 16 bits) */
+    FA_ERR_DIM = 2,          /* a size is < 1, an index would overflow int64, or Nk is above 2^31 - 256 (without
+                              * a window decode takes up to 2^31 - 32, and pages of 16 bits any) */
     FA_ERR_GQA_RATIO = 3,    /* Hq is not a multiple of Hkv */
     FA_ERR_HEAD_DIM = 4,     /* D unsupported: D % 8 != 0 or D > 256 */
     FA_ERR_CAUSAL_SHAPE = 5, /* causal with Nq > Nk */

@@ -152,12 +152,14 @@ int decode_splits(int B, int Hq, int Hkv, int Nk, int D, const Window &w, bool m
 }
 
 // Most keys of a call: the kernels count keys in ints, up to the end of the last tile of
-// at most 128, and a tile ahead.  Without a window the decode kernel has no such end,
-// and pages, 64 keys at least, end 64 ahead of 2^31: enough for the 16-bit kernels' tiles.
+// at most 128, a tile ahead, and a window's length behind a row of the 128 before a
+// tile.  Without a window the decode kernel's chunks of 32 need only their own end, and
+// pages, of 64 keys at least, stop 64 ahead of 2^31: enough for the 16-bit kernels' tiles.
 constexpr int kMostKeys = 0x7fffffff - 255;
 bool keys_fit(int Nk, bool decode, bool prefill, bool paged, bool windowed) {
     if (Nk <= kMostKeys) return true;
-    return paged ? decode || prefill : decode && !windowed;
+    if (windowed) return false;
+    return paged ? decode || prefill : decode && Nk <= 0x7fffffff - 31;
 }
 
 struct Paging {

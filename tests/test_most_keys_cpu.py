@@ -30,7 +30,16 @@ def test_all_keys(Nq, D, it):
 
 
 def test_decode_takes_them():
-    assert validate(*A[:5], 1, 1, 1, 1, 2**31 - 1, 64, 0, 0.5, "f16") == 0
+    """To the end of its last chunk of 32."""
+    assert validate(*A[:5], 1, 1, 1, 1, 2**31 - 32, 64, 0, 0.5, "f16") == 0
+    assert validate(*A[:5], 1, 1, 1, 1, 2**31 - 31, 64, 0, 0.5, "f16") == 2
+
+
+@pytest.mark.parametrize("Nq", [1, 9])
+def test_windows_of_pages(Nq):
+    lib = _lib.load()
+    args = [*A[:5], A[7], A[8], 1, 1, 1, Nq, 64, 64, 2**25 - 1, 1, 2**31 - 1, 4, 0.5, None, 0, 0, A[6], 1 << 30]
+    assert lib.fa_fwd_window_paged(*args) == 2
 
 
 def test_pages_of_long_rows():
